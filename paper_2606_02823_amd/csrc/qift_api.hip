@@ -146,6 +146,8 @@ uint32_t* device_error_word() {
   return g_err_word[dev];
 }
 
+int report_hip(hipError_t e) { return hip_status(e); }
+
 int wait_limit() { return g_wait_limit.load(std::memory_order_relaxed); }
 
 }  // namespace qift

@@ -40,6 +40,41 @@ hipError_t launch_kv4_attention(const uint16_t* q, int64_t B, int Hq, int Hkv, i
                                 const uint8_t* kc, const float* ks, const uint8_t* kz, const uint8_t* vc,
                                 const float* vs, const uint8_t* vz, uint16_t* y, void* ws, hipStream_t s);
 
+// The paged KV4 cache (qift_pages.hip, qift_tree.hip): rows [pages][Hkv][page] of 64 code bytes, a scale and a
+// zero-point, for keys and values.  Element types as QIFT_F16, QIFT_BF16, QIFT_F32; kDevErrIndex is QIFT_DEVERR_INDEX.
+constexpr int kF16 = 0, kBF16 = 1, kF32 = 2;
+constexpr uint32_t kDevErrIndex = 4;
+struct Kv4Pool {
+  int64_t pages;
+  int32_t page, Hkv;
+  uint8_t* kc;
+  float* ks;
+  uint8_t* kz;
+  uint8_t* vc;
+  float* vs;
+  uint8_t* vz;
+};
+hipError_t launch_kv4_append(const Kv4Pool& c, const uint16_t* k, const uint16_t* v, int64_t ks, int64_t vs, int dtype,
+                             const int32_t* slots, int64_t n, uint16_t* kv, uint16_t* vv, hipStream_t s);
+hipError_t launch_kv4_read(const Kv4Pool& c, const int32_t* slots, int64_t n, int dtype, void* ko, void* vo,
+                           hipStream_t s);
+// Attention of up to max_nodes new tokens per sequence; ws as pages::records asks (qift_pages.h).
+struct TreeCall {
+  Kv4Pool c;
+  const uint16_t* q;
+  int64_t q_stride, rows, B, max_len;
+  const int32_t* table;
+  const int32_t* starts;
+  const int32_t* lens;
+  const uint64_t* visible;
+  uint16_t* out;
+  float* ws;
+  int32_t table_pages, Hq, max_nodes, dtype;
+};
+hipError_t launch_kv4_tree(const TreeCall& a, hipStream_t s);
+// The status of a HIP call, kept for qift_last_hip_error (qift_api.hip)
+int report_hip(hipError_t e);
+
 // Linear over a four-level fp16 table (qift_lut.hip): lut holds the table entries exactly
 hipError_t launch_lut_linear(const uint32_t* packed, const uint16_t* scales, int64_t N, int64_t K, const double lut[4],
                              const int8_t* act_q, const float* act_scale, int64_t M, uint16_t* out, hipStream_t s);

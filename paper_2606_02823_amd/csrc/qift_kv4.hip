@@ -29,14 +29,13 @@
 // large copy's rate), B = 1 9.0 -> 8.0.
 #include "qift_fwht.h"
 #include "qift_internal.h"
+#include "qift_kv4_group.h"
 
 namespace qift {
 namespace {
 
-constexpr int kD = 128;         // head dimension
 constexpr int kChunk = 256;     // cached tokens per workgroup
 
-typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef int v2i __attribute__((ext_vector_type(2)));
@@ -71,39 +70,6 @@ __device__ __forceinline__ v8h codes_minus_z(uint32_t w, v2h base) {
   return v8h{h0[0], h0[1], h1[0], h1[1], h2[0], h2[1], h3[0], h3[1]};
 }
 
-// Reductions by DPP moves within rows of 16 lanes (every lane gets its row's result) and lane reads across
-// the four rows: a few cycles a step, where a shuffle through LDS takes about a hundred.
-#define QIFT_DPP_B32(x, CTRL) __builtin_amdgcn_update_dpp(x, x, CTRL, 0xf, 0xf, false)
-template <typename Op>
-__device__ __forceinline__ int row_reduce(int x, Op op) {
-  x = op(x, QIFT_DPP_B32(x, 0xb1));    // quad_perm [1,0,3,2]
-  x = op(x, QIFT_DPP_B32(x, 0x4e));    // quad_perm [2,3,0,1]
-  x = op(x, QIFT_DPP_B32(x, 0x141));   // row_half_mirror
-  return op(x, QIFT_DPP_B32(x, 0x140));   // row_mirror
-}
-
-template <typename Op>
-__device__ __forceinline__ float wave_reduce(float x, Op op) {   // every lane gets the wave's result
-  const int r = row_reduce(__float_as_int(x), [&](int a, int b) {
-    return __float_as_int(op(__int_as_float(a), __int_as_float(b)));
-  });
-  auto row = [&](int l) { return __int_as_float(__builtin_amdgcn_readlane(r, l)); };
-  return op(op(row(0), row(16)), op(row(32), row(48)));
-}
-__device__ __forceinline__ float max_op(float a, float b) { return fmaxf(a, b); }
-__device__ __forceinline__ float add_op(float a, float b) { return a + b; }
-
-__device__ __forceinline__ v2h pk_max(v2h a, v2h b) { return __builtin_elementwise_max(a, b); }
-
-// d / 15 correctly rounded for a finite d >= 0 that is 0 or far above the subnormals (the values here are
-// fp16 times 0.95): the quotient by the rounded reciprocal, then one correction (checked against the
-// division for every fp32 mantissa).
-__device__ __forceinline__ float div15(float d) {
-  constexpr float y = 1.0f / 15.0f;
-  const float q = d * y;
-  return d == INFINITY ? d : fmaf(fmaf(-q, 15.0f, d), y, q);
-}
-
 // Bound by its arithmetic: 25 vector instructions a value took 85 % of the cycles (3.3 TB/s at 524288
 // groups).  So the maxima run on packed fp16 pairs (max x and max -x in one register through the row
 // moves), the reciprocal is the hardware's approximation (the residual test decides as before), one
@@ -128,55 +94,12 @@ __global__ __launch_bounds__(256) void k_kv4_quant(const uint16_t* __restrict__ 
     const int64_t grp = wq * 4 + (lane >> 4);
     const uint4 u = next;
     if (i + 1 < per) next = load(wq + 4);
-    const v2h h[4] = {__builtin_bit_cast(v2h, u.x), __builtin_bit_cast(v2h, u.y), __builtin_bit_cast(v2h, u.z),
-                      __builtin_bit_cast(v2h, u.w)};
-    float v[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = (float)h[e >> 1][e & 1];
-    // (max x, max -x) of the lane, then of its group's 16 lanes
-    const v2h hx = pk_max(pk_max(h[0], h[1]), pk_max(h[2], h[3]));
-    const v2h hn = pk_max(pk_max(-h[0], -h[1]), pk_max(-h[2], -h[3]));
-    const v2h both = pk_max(v2h{hx[0], hn[0]}, v2h{hx[1], hn[1]});
-    const v2h ext = __builtin_bit_cast(v2h, row_reduce(__builtin_bit_cast(int, both), [](int a, int b) {
-                                         return __builtin_bit_cast(int, pk_max(__builtin_bit_cast(v2h, a), __builtin_bit_cast(v2h, b)));
-                                       }));
-    const float c = 0.95f;
-    const float x_max = fmaxf((float)ext[0], 0.f) * c, x_min = fminf(-(float)ext[1], 0.f) * c;
-    float s = div15(x_max - x_min);
-    if (s == 0.f) s = 1.f;
-    // rint of the rounded quotient v / s without the division where it is clear: q0 = rint(v r), r the
-    // approximate reciprocal, is that value when the residual v - q0 s lies inside half a step by more
-    // than both roundings (|v / s| < 32 here); otherwise (a wave-uniform branch, rarely taken) divide.
-    // The zero-point is decided the same way.
-    const float inv = __builtin_amdgcn_rcpf(s);
-    float qf[8];
-    float z = rintf(-x_min * inv);
-    float res = fabsf(fmaf(-z, s, -x_min));
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      qf[e] = rintf(v[e] * inv);
-      res = fmaxf(res, fabsf(fmaf(-qf[e], s, v[e])));
-    }
-    const float half = (0.5f - 0x1p-16f) * s;
-    if (__any(!(res < half))) {
-      z = rintf(-x_min / s);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) qf[e] = rintf(v[e] / s);
-    }
-    z = fminf(fmaxf(z, 0.f), 15.f);
-    // codes as bytes, even values and odd ones, then two to a byte: values 8j .. 8j + 7
-    uint32_t even = 0, odd = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float q = fminf(fmaxf(qf[e] + z, 0.f), 15.f);
-      if (e & 1) odd = __builtin_amdgcn_cvt_pk_u8_f32(q, e >> 1, odd);
-      else even = __builtin_amdgcn_cvt_pk_u8_f32(q, e >> 1, even);
-    }
+    const Kv4Group g = kv4_group<false>(u);
     if (grp < groups) {
-      reinterpret_cast<uint32_t*>(codes + grp * (kD / 2))[j] = even | (odd << 4);
+      reinterpret_cast<uint32_t*>(codes + grp * (kD / 2))[j] = g.codes();
       if (j == 0) {
-        scales[grp] = s;
-        zeros[grp] = (uint8_t)z;
+        scales[grp] = g.s;
+        zeros[grp] = (uint8_t)g.z;
       }
     }
   }

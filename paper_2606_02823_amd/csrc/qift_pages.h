@@ -1,0 +1,117 @@
+// Index arithmetic of the paged KV4 cache and of the attention over it, for the kernels and for host code
+// (plain C++: compiled without a GPU too).
+#pragma once
+
+#include <stdint.h>
+
+#ifdef __HIPCC__
+#define QIFT_HD __host__ __device__ __forceinline__
+#else
+#define QIFT_HD inline
+#endif
+
+namespace qift {
+namespace pages {
+
+// Division of x < 2^31 by a fixed d, 1 <= d < 2^31: with 2^s >= d the multiplier m = ceil(2^(31 + s) / d) has at most
+// 32 bits and floor(x m / 2^(31 + s)) = floor(x / d) for every x below 2^31 (m d - 2^(31 + s) < d <= 2^s).
+struct Div {
+  uint32_t d, m, s;   // s: the shift left after the high word of the product
+};
+inline Div make_div(uint32_t d) {
+  uint32_t s = 1;
+  while (s < 31 && (uint32_t(1) << s) < d) ++s;
+  if (d == 1) return {1, 0, 0};
+  return {d, (uint32_t)(((uint64_t(1) << (31 + s)) + d - 1) / d), s - 1};
+}
+QIFT_HD uint32_t quotient(uint32_t x, Div v) {
+  return v.d == 1 ? x : (uint32_t)(((uint64_t)x * v.m) >> 32) >> v.s;
+}
+
+// Row of a slot: rows are [pages][Hkv][page].  The caller has checked 0 <= slot < pages * page; rows stay below 2^31.
+QIFT_HD uint32_t slot_row(uint32_t slot, Div page, uint32_t Hkv, uint32_t head) {
+  const uint32_t p = quotient(slot, page);
+  return (p * Hkv + head) * page.d + (slot - p * page.d);
+}
+
+// Row of token t of a sequence whose table entry for that token is `entry` (checked to name a page); tiles divides by the
+// 16-token tiles of a page.
+QIFT_HD uint32_t table_index(uint32_t t, Div tiles) { return quotient(t >> 4, tiles); }
+QIFT_HD uint32_t token_row(uint32_t t, uint32_t entry, uint32_t Hkv, uint32_t head, Div tiles) {
+  const uint32_t page = tiles.d * 16;
+  return (entry * Hkv + head) * page + (t - table_index(t, tiles) * page);
+}
+
+// Nodes and tokens of one sequence, taken from device data that may hold anything: every count is brought into the
+// range the launch was made for, and bad says that one was not.
+struct Seq {
+  int32_t row0, n, len, ctx;   // first row of q, rows, cached tokens, tokens before the first node
+  bool bad;
+};
+QIFT_HD Seq sequence(int32_t s0, int32_t s1, int32_t len, int32_t rows, int32_t max_nodes, int64_t most) {
+  Seq q;
+  q.bad = s0 < 0 || s1 < s0 || s1 > rows || len < 0 || (int64_t)len > most;
+  q.row0 = s0 < 0 ? 0 : s0 > rows ? rows : s0;
+  const int32_t end = s1 < q.row0 ? q.row0 : s1 > rows ? rows : s1;
+  q.n = end - q.row0;
+  if (q.n > max_nodes) {
+    q.n = max_nodes;
+    q.bad = true;
+  }
+  q.len = len < 0 ? 0 : (int64_t)len > most ? (int32_t)most : len;
+  q.ctx = q.len > q.n ? q.len - q.n : 0;
+  return q;
+}
+
+// Tokens that the block of query rows [block_rows block, block_rows (block + 1)) reaches: without a mask a row sees
+// nothing past its own node.
+QIFT_HD int32_t last_token(const Seq& q, bool masked, Div group, int32_t block_rows, int32_t block) {
+  if (masked) return q.len;
+  int32_t node = (int32_t)quotient((uint32_t)((block + 1) * block_rows - 1), group);
+  if (node > q.n - 1) node = q.n - 1;
+  const int32_t end = q.ctx + node + 1;
+  return end < q.len ? end : q.len;
+}
+
+// Which of the 64 tokens t0 .. t0 + 63 row `node` sees, without the end of the sequence: bit i is token t0 + i.
+QIFT_HD uint64_t low_bits(int32_t n) { return n <= 0 ? 0 : n >= 64 ? ~uint64_t(0) : (uint64_t(1) << n) - 1; }
+QIFT_HD uint64_t chain_bits(int32_t t0, int32_t ctx, int32_t node) { return low_bits(ctx + node + 1 - t0); }
+// From the words of the row's mask: d0 = t0 - ctx is the node at token t0 (negative: tokens before the first node, all
+// seen); w0 is mask word max(d0, 0) / 64 and w1 the next, 0 past the mask's words.
+QIFT_HD uint64_t tree_bits(int32_t d0, uint64_t w0, uint64_t w1) {
+  if (d0 <= -64) return ~uint64_t(0);
+  if (d0 < 0) return low_bits(-d0) | (w0 << -d0);
+  const int32_t sh = d0 & 63;
+  return sh ? (w0 >> sh) | (w1 << (64 - sh)) : w0;
+}
+
+// How the attention cuts its work: a workgroup takes rt tiles of 16 query rows (a row is a node and a head of the
+// KV head's group) over one chunk of tokens; four waves share the chunk in steps of 64 tokens.
+constexpr int kStep = 64, kWaves = 4, kRound = kStep * kWaves;
+struct Plan {
+  int32_t rt, blocks;     // row tiles of a workgroup, workgroups over a KV head's rows
+  int32_t chunk, chunks;  // tokens of a chunk (a multiple of kRound), chunks of the longest sequence
+};
+inline Plan plan(int64_t B, int32_t Hkv, int32_t G, int32_t max_nodes, int64_t max_len) {
+  Plan p;
+  const int64_t rows = (int64_t)max_nodes * G;
+  p.rt = rows <= 16 ? 1 : 2;
+  p.blocks = (int32_t)((rows + 16 * p.rt - 1) / (16 * p.rt));
+  const int64_t units = B * Hkv * p.blocks, rounds = (max_len + kRound - 1) / kRound;
+  const int64_t target = p.rt == 1 ? 1024 : 512;
+  int64_t want = (target + units - 1) / units;
+  if (want > rounds) want = rounds;
+  if (want < 1) want = 1;
+  const int64_t per = rounds < 1 ? 1 : (rounds + want - 1) / want;
+  p.chunk = (int32_t)(per * kRound);
+  p.chunks = (int32_t)(rounds < 1 ? 1 : (rounds + per - 1) / per);
+  return p;
+}
+// Partial records: per (sequence, KV head, chunk, row) 128 sums, then (after all sums) the running maximum and the sum of
+// exponentials.
+inline int64_t records(const Plan& p, int64_t B, int32_t Hkv, int32_t G, int32_t max_nodes) {
+  return p.chunks == 1 ? 0 : B * Hkv * p.chunks * ((int64_t)max_nodes * G);
+}
+
+}  // namespace pages
+}  // namespace qift

@@ -27,6 +27,7 @@ STATUS = {0: "QIFT_OK", -1: "QIFT_ERR_NULL", -2: "QIFT_ERR_SHAPE", -3: "QIFT_ERR
           -4: "QIFT_ERR_FORMAT", -5: "QIFT_ERR_CODE", -6: "QIFT_ERR_ALIGN", -7: "QIFT_ERR_HIP",
           -8: "QIFT_ERR_WORKSPACE"}
 DEVERR_GROUP_WAIT, DEVERR_CHAIN_WAIT = 1, 2   # bits of the device error word (qift_device_error)
+DEVERR_INDEX = 4   # QIFT_DEVERR_INDEX: a slot, page, count or length outside its range (paged cache)
 
 # every symbol declared in include/qift.h
 EXPORTS = ("qift_packed_bytes", "qift_pack_w2", "qift_pack_w4", "qift_quantize_weights",
@@ -37,6 +38,9 @@ EXPORTS = ("qift_packed_bytes", "qift_pack_w2", "qift_pack_w4", "qift_quantize_w
            "qift_rotate_quant_linear", "qift_hbm_read_probe", "qift_workspace_bytes", "qift_status_string",
            "qift_last_hip_error", "qift_device_error", "qift_set_wait_limit", "qift_chain_workspace_bytes",
            "qift_chain_prepare", "qift_decode_chain", "qift_version")
+
+# every symbol declared in include/qift_pages.h
+PAGES_EXPORTS = ("qift_kv4_append", "qift_kv4_read", "qift_kv4_attention_tree_workspace_bytes", "qift_kv4_attention_tree")
 
 
 class QiftError(RuntimeError):
@@ -81,6 +85,13 @@ class ChainC(ctypes.Structure):
     _fields_ = [("fmt", ctypes.c_int32), ("n_links", ctypes.c_int32), ("M", ctypes.c_int32), ("K0", ctypes.c_int32),
                 ("grid", ctypes.c_int32), ("kmax", ctypes.c_int32), ("region0", ctypes.c_int32),
                 ("reserved", ctypes.c_int32), ("table", ctypes.c_void_p), ("counters", ctypes.c_void_p)]
+
+
+class KV4PagesC(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_int64), ("page", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("k_codes", ctypes.c_void_p), ("k_scales", ctypes.c_void_p),
+                ("k_zeros", ctypes.c_void_p), ("v_codes", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
+                ("v_zeros", ctypes.c_void_p)]
 
 
 _lib = None
@@ -128,6 +139,11 @@ def lib():
                                               vp]),
         "qift_decode_chain": (ctypes.c_int, [ctypes.POINTER(ChainC), vp, vp]),
         "qift_version": (ctypes.c_char_p, []),
+        "qift_kv4_append": (ctypes.c_int, [vp, vp, vp, i64, i64, i32, vp, i64, vp, vp, vp]),
+        "qift_kv4_read": (ctypes.c_int, [vp, vp, i64, i32, vp, vp, vp]),
+        "qift_kv4_attention_tree_workspace_bytes": (sz, [i64, i32, i32, i32, i32, i64]),
+        "qift_kv4_attention_tree": (ctypes.c_int, [vp, vp, i64, i32, i64, vp, i32, vp, vp, i64, i32, i32, i64, vp, vp, vp,
+                                                   sz, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -395,6 +411,178 @@ def kv4_attention_decode_noalloc(q: torch.Tensor, k: KV4, v: KV4, out: torch.Ten
                                                  v.codes.data_ptr(), v.scales.data_ptr(), v.zeros.data_ptr(),
                                                  out.data_ptr(), _stream(stream))
     _check("qift_kv4_attention_decode_noalloc", st)
+    return out
+
+
+_DTYPE = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}   # QIFT_F16, QIFT_BF16, QIFT_F32
+
+
+class KV4Pages:
+    """A paged KV4 cache (qift_kv4_pages): keys k and values v as KV4 tensors of rows [pages, Hkv, page], i.e. codes
+    uint8 [pages, Hkv, page, 64], scales fp32 and zeros uint8 [pages, Hkv, page].  Slot p * page + i is token i of
+    page p.  The object keeps the tensors alive and holds the C view, checked once here."""
+
+    def __init__(self, k: KV4, v: KV4):
+        if k.codes.dim() != 4:
+            raise ValueError("codes must have shape [pages, Hkv, page, 64]")
+        rows = tuple(k.codes.shape[:3])
+        for name, c in (("k", k), ("v", v)):
+            _dev(c.codes, torch.uint8, rows + (64,), name + ".codes")
+            _dev(c.scales, torch.float32, rows, name + ".scales")
+            _dev(c.zeros, torch.uint8, rows, name + ".zeros")
+        _same_device(k.codes, (k.scales, k.zeros, v.codes, v.scales, v.zeros))
+        self.k, self.v = k, v
+        self.pages, self.Hkv, self.page = rows
+        self.device = k.codes.device
+        self.c = KV4PagesC(self.pages, self.page, self.Hkv, 128, 0, k.codes.data_ptr(), k.scales.data_ptr(),
+                           k.zeros.data_ptr(), v.codes.data_ptr(), v.scales.data_ptr(), v.zeros.data_ptr())
+        self._ref = ctypes.byref(self.c)
+
+    @classmethod
+    def empty(cls, pages: int, page: int, Hkv: int, device="cuda") -> "KV4Pages":
+        """A pool of pages that no token has been written to (every scale 0, so that unwritten rows read as zeros)."""
+        rows = (pages, Hkv, page)
+        return cls(*(KV4(torch.zeros(rows + (64,), dtype=torch.uint8, device=device),
+                         torch.zeros(rows, dtype=torch.float32, device=device),
+                         torch.zeros(rows, dtype=torch.uint8, device=device)) for _ in range(2)))
+
+
+def _same_device(t, others):
+    for o in others:
+        if o is not None and o.device != t.device:
+            raise ValueError(f"tensors on {t.device} and {o.device}: one call takes one device")
+
+
+def _empty(shape, dtype, device, stream=None) -> torch.Tensor:
+    """Memory for a call on `stream`: taken from that stream's pool, so that what is freed here is not reused by
+    another stream while the call runs."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _rows(t: torch.Tensor, dtype, heads: int, name: str) -> int:
+    """The row stride of a [rows, heads, 128] view whose rows are contiguous (a part of stacked rows, say)."""
+    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != 128:
+        raise ValueError(f"{name} must have shape (rows, {heads}, 128), got {tuple(t.shape)}")
+    n, stride = t.shape[0], t.stride()
+    if n and (stride[2] != 1 or (heads > 1 and stride[1] != 128)):
+        raise ValueError(f"{name} must have contiguous rows")
+    return stride[0] if n > 1 else heads * 128
+
+
+class _on:
+    """Makes a tensor's device the current one for a call, where it is not already (the kernels are launched on the
+    current device and its current stream)."""
+
+    def __init__(self, device):
+        self.other = None
+        if device.index is not None and device.index != torch.cuda.current_device():
+            self.other = torch.cuda.device(device)
+
+    def __enter__(self):
+        if self.other is not None:
+            self.other.__enter__()
+
+    def __exit__(self, *exc):
+        if self.other is not None:
+            self.other.__exit__(*exc)
+
+
+def kv4_append(cache: KV4Pages, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, values=False, stream=None):
+    """Quantize the keys and values of n new tokens (fp16 or bf16 [n, Hkv, 128], row-strided views taken as they
+    are) into their slots (int32 [n]; negative: not written).  values=True, or a pair of tensors [n, Hkv, 128] to
+    write: returns (k, v) as the cache now stands for them, else None.  A slot may appear once in a call."""
+    dt = k.dtype
+    if dt not in (torch.float16, torch.bfloat16):
+        raise TypeError(f"k must be torch.float16 or torch.bfloat16, got {dt}")
+    ks, vs = _rows(k, dt, cache.Hkv, "k"), _rows(v, dt, cache.Hkv, "v")
+    n = k.shape[0]
+    if v.shape[0] != n:
+        raise ValueError(f"k has {n} rows, v {v.shape[0]}")
+    _dev(slots, torch.int32, (n,), "slots")
+    out = (None, None)
+    if values is True:
+        out = tuple(_empty((n, cache.Hkv, 128), dt, k.device, stream) for _ in range(2))
+    elif values is not False and values is not None:
+        out = tuple(values)
+        for t in out:
+            _dev(t, dt, (n, cache.Hkv, 128), "values")
+    _same_device(cache.k.codes, (k, v, slots, *out))
+    with _on(cache.device):
+        st = lib().qift_kv4_append(cache._ref, k.data_ptr(), v.data_ptr(), ks, vs, _DTYPE[dt], slots.data_ptr(), n,
+                                   _ptr(out[0]), _ptr(out[1]), _stream(stream))
+    _check("qift_kv4_append", st)
+    return None if out[0] is None else out
+
+
+def kv4_read(cache: KV4Pages, slots: torch.Tensor, dtype=torch.float16, out=None, stream=None):
+    """(k, v) [n, Hkv, 128] of the given slots (int32 [n]; negative: zeros) in dtype fp16, bf16 or fp32."""
+    if dtype not in _DTYPE:
+        raise TypeError(f"dtype must be torch.float16, torch.bfloat16 or torch.float32, got {dtype}")
+    n = slots.numel()
+    _dev(slots, torch.int32, (n,), "slots")
+    if out is None:
+        out = tuple(_empty((n, cache.Hkv, 128), dtype, cache.device, stream) for _ in range(2))
+    for t in out:
+        _dev(t, dtype, (n, cache.Hkv, 128), "out")
+    _same_device(cache.k.codes, (slots, *out))
+    with _on(cache.device):
+        st = lib().qift_kv4_read(cache._ref, slots.data_ptr(), n, _DTYPE[dtype], out[0].data_ptr(), out[1].data_ptr(),
+                                 _stream(stream))
+    _check("qift_kv4_read", st)
+    return out
+
+
+def kv4_attention_tree_workspace(B: int, Hq: int, Hkv: int, max_nodes: int, max_len: int, device="cuda") -> torch.Tensor:
+    """A workspace for kv4_attention_tree calls with these limits (one call at a time)."""
+    need = int(lib().qift_kv4_attention_tree_workspace_bytes(B, Hq, Hkv, 128, max_nodes, max_len))
+    return torch.empty(max(need, 16), dtype=torch.uint8, device=device)
+
+
+def kv4_attention_tree(q: torch.Tensor, cache: KV4Pages, table: torch.Tensor, starts: torch.Tensor, lens: torch.Tensor,
+                       max_nodes: int, max_len: int, visible: torch.Tensor | None = None, out=None, workspace=None,
+                       stream=None) -> torch.Tensor:
+    """Attention of the new tokens of B sequences over their pages: q fp16 or bf16 [rows, Hq, 128] (row-strided views
+    taken as they are), sequence b's rows starts[b] .. starts[b+1] - 1 (int32 [B + 1]) being the last of its lens[b]
+    cached tokens (int32 [B]) in the pages table[b] (int32 [B, table_pages]).  visible (int64 [rows,
+    ceil(max_nodes / 64)]): bit j of a row says that it sees node j of its sequence; None: nodes up to its own.
+    Returns [rows, Hq, 128] in q's type."""
+    dt = q.dtype
+    if dt not in (torch.float16, torch.bfloat16):
+        raise TypeError(f"q must be torch.float16 or torch.bfloat16, got {dt}")
+    if q.dim() != 3:
+        raise ValueError(f"q must have shape (rows, Hq, 128), got {tuple(q.shape)}")
+    rows, Hq = q.shape[0], q.shape[1]
+    qs = _rows(q, dt, Hq, "q")
+    if not isinstance(table, torch.Tensor) or table.dim() != 2:
+        raise ValueError("table must have shape (B, table_pages)")
+    B = table.shape[0]
+    _dev(table, torch.int32, (B, table.shape[1]), "table")
+    _dev(starts, torch.int32, (B + 1,), "starts")
+    _dev(lens, torch.int32, (B,), "lens")
+    if visible is not None:
+        _dev(visible, torch.int64, (rows, (max_nodes + 63) // 64), "visible")
+    if out is None:
+        out = _empty((rows, Hq, 128), dt, q.device, stream)
+    _dev(out, dt, (rows, Hq, 128), "out")
+    if workspace is None:
+        need = int(lib().qift_kv4_attention_tree_workspace_bytes(B, Hq, cache.Hkv, 128, max_nodes, max_len))
+        workspace = _empty(max(need, 16), torch.uint8, q.device, stream)
+    else:
+        _dev(workspace, torch.uint8, (workspace.numel(),), "workspace")
+    _same_device(cache.k.codes, (q, table, starts, lens, visible, out, workspace))
+    with _on(cache.device):
+        st = lib().qift_kv4_attention_tree(cache._ref, q.data_ptr(), qs, _DTYPE[dt], rows, table.data_ptr(),
+                                           table.shape[1], starts.data_ptr(), lens.data_ptr(), B, Hq, max_nodes, max_len,
+                                           _ptr(visible), out.data_ptr(), workspace.data_ptr(), workspace.numel(),
+                                           _stream(stream))
+    _check("qift_kv4_attention_tree", st)
     return out
 
 
