@@ -85,33 +85,40 @@ QIFT_HD uint64_t tree_bits(int32_t d0, uint64_t w0, uint64_t w1) {
   return sh ? (w0 >> sh) | (w1 << (64 - sh)) : w0;
 }
 
-// How the attention cuts its work: a workgroup takes rt tiles of 16 query rows (a row is a node and a head of the
-// KV head's group) over one chunk of tokens; four waves share the chunk in steps of 64 tokens.
+// How the attention cuts its work.  A workgroup takes a block of 16 rt query rows (a row is a node and a head of the KV
+// head's group) of one KV head and sequence at a time (a unit), over tokens in rounds of 256: 64 for each of its four
+// waves.  Few units: the rounds of all units, in order, are dealt out evenly to `shares` workgroups a block of rows, whatever the
+// sequences' lengths are; a unit that more than one share covers is joined from partial records.  Many units: one
+// workgroup takes a unit whole.
 constexpr int kStep = 64, kWaves = 4, kRound = kStep * kWaves;
+constexpr int kMostShared = 512;   // sequences whose rounds are dealt out (every workgroup adds them up)
 struct Plan {
-  int32_t rt, blocks;     // row tiles of a workgroup, workgroups over a KV head's rows
-  int32_t chunk, chunks;  // tokens of a chunk (a multiple of kRound), chunks of the longest sequence
+  int32_t rt, blocks;   // row tiles of a workgroup, blocks of a KV head's rows
+  int32_t shares;       // workgroups of a block of rows; 0: one to a unit
 };
+QIFT_HD int32_t rounds_of(int32_t len) { return len < 1 ? 1 : (int32_t)(((int64_t)len + kRound - 1) / kRound); }
 inline Plan plan(int64_t B, int32_t Hkv, int32_t G, int32_t max_nodes, int64_t max_len) {
   Plan p;
   const int64_t rows = (int64_t)max_nodes * G;
   p.rt = rows <= 16 ? 1 : 2;
   p.blocks = (int32_t)((rows + 16 * p.rt - 1) / (16 * p.rt));
-  const int64_t units = B * Hkv * p.blocks, rounds = (max_len + kRound - 1) / kRound;
-  const int64_t target = p.rt == 1 ? 1024 : 512;
-  int64_t want = (target + units - 1) / units;
-  if (want > rounds) want = rounds;
-  if (want < 1) want = 1;
-  const int64_t per = rounds < 1 ? 1 : (rounds + want - 1) / want;
-  p.chunk = (int32_t)(per * kRound);
-  p.chunks = (int32_t)(rounds < 1 ? 1 : (rounds + per - 1) / per);
+  const int64_t units = B * Hkv, rounds = (max_len + kRound - 1) / kRound;
+  p.shares = 0;
+  if (rounds > 1 && B <= kMostShared && units * p.blocks < 1024) {
+    int64_t n = 512 / p.blocks;                 // two workgroups to each of 256 CUs
+    if (n > units * rounds) n = units * rounds;
+    p.shares = n < 1 ? 1 : (int32_t)n;
+  }
   return p;
 }
-// Partial records: per (sequence, KV head, chunk, row) 128 sums, then (after all sums) the running maximum and the sum of
-// exponentials.
-inline int64_t records(const Plan& p, int64_t B, int32_t Hkv, int32_t G, int32_t max_nodes) {
-  return p.chunks == 1 ? 0 : B * Hkv * p.chunks * ((int64_t)max_nodes * G);
-}
+// Share i of n covers the rounds [first_round(i), first_round(i + 1)) of W; round r lies in share_of(r).  No share is
+// empty: there are at most as many as rounds.
+QIFT_HD int32_t used_shares(int64_t W, int32_t shares) { return W < shares ? (int32_t)W : shares; }
+QIFT_HD int64_t first_round(int64_t W, int32_t n, int32_t i) { return W * i / n; }
+QIFT_HD int32_t share_of(int64_t W, int32_t n, int64_t r) { return (int32_t)(((r + 1) * n - 1) / W); }
+// Partial records: share i and unit u have number i + u (both grow along the rounds, so no two have the same), each
+// 128 sums per row, then (after all sums) the rows' references and sums of exponentials.
+inline int64_t records(const Plan& p, int64_t B, int32_t Hkv) { return p.shares == 0 ? 0 : p.shares + B * Hkv; }
 
 }  // namespace pages
 }  // namespace qift

@@ -35,9 +35,8 @@ qift::Kv4Pool pool(const qift_kv4_pages* c) {
 bool tree_shape_ok(int64_t B, int32_t Hq, int32_t Hkv, int32_t head_dim, int32_t max_nodes, int64_t max_len) {
   if (head_dim != 128 || B < 0 || B > 65535 || Hkv < 1 || Hkv > 65535 || Hq < Hkv || Hq % Hkv || Hq / Hkv > 64) return false;
   if (max_nodes < 1 || max_nodes > 256 || max_len < 1 || max_len >= (int64_t(1) << 28)) return false;
-  // the launch: one workgroup to a chunk, KV head, sequence and block of rows
   const qift::pages::Plan p = qift::pages::plan(B < 1 ? 1 : B, Hkv, Hq / Hkv, max_nodes, max_len);
-  return (B * Hkv * p.chunks + 8) * p.blocks < k31;
+  return ((p.shares ? p.shares : B * Hkv) + 8) * p.blocks < k31;
 }
 
 }  // namespace
@@ -82,7 +81,7 @@ size_t qift_kv4_attention_tree_workspace_bytes(int64_t B, int32_t Hq, int32_t Hk
                                                int64_t max_len) {
   if (!tree_shape_ok(B, Hq, Hkv, head_dim, max_nodes, max_len) || B == 0) return 0;
   const qift::pages::Plan p = qift::pages::plan(B, Hkv, Hq / Hkv, max_nodes, max_len);
-  return (size_t)qift::pages::records(p, B, Hkv, Hq / Hkv, max_nodes) * 130 * sizeof(float);
+  return (size_t)qift::pages::records(p, B, Hkv) * ((size_t)max_nodes * (Hq / Hkv)) * 130 * sizeof(float);
 }
 
 int qift_kv4_attention_tree(const qift_kv4_pages* cache, const void* q, int64_t q_stride, int32_t dtype, int64_t rows,

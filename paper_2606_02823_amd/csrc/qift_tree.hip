@@ -2,10 +2,11 @@
 // paged KV4 cache:
 //   out[row][h] = sum_t p_t v_t,  p = softmax over the tokens the row sees of q . k_t / sqrt(128),
 //   k_t = s_t (code - z_t) and v_t likewise.
-// A KV head's query rows are its nodes times the G heads of its group.  Workgroup (chunk, KV head and sequence, block of
-// rows) takes 16 RT rows over one chunk of tokens; its four waves take every fourth step of 64 tokens each, keep their own
-// running maximum, sum of exponentials and output sums in registers, and meet once at the end, so the loop has no
-// barrier and a step's codes are unpacked once for all rows.  Chunks of a long sequence are joined by k_tree_merge.
+// A KV head's query rows are its nodes times the G heads of its group.  A workgroup takes 16 RT rows over a run of tokens
+// of one sequence; its four waves take every fourth step of 64 tokens each, keep their own reference, sum of
+// exponentials and output sums in registers, and meet once at the run's end, so the loop has no barrier and a step's
+// codes are unpacked once for all rows.  The runs are even shares of all sequences' tokens (pages::Plan); those of one
+// sequence are joined by k_tree_merge.
 //
 // Per step, with c = lane mod 16 and kg = lane / 16:
 //   scores   D[token][row] on the f16 MFMA, A = 16 tokens x 32 dimensions of code - z (exact), B = the queries; lane
@@ -17,8 +18,6 @@
 //   values   D[dimension][row] += A[dimension][token] B[token][row], B = w as two fp16 parts (2^-21 relative), which the
 //            lane holds in place: the contraction's order of tokens is the one the scores left, and the transposing
 //            LDS read is given the rows of the lane's own 16 tokens, so no weight crosses lanes.
-#include <type_traits>
-
 #include "qift_fwht.h"
 #include "qift_internal.h"
 #include "qift_kv4_group.h"
@@ -66,24 +65,71 @@ struct TreeArgs {
   uint16_t* out;
   float* part;
   uint32_t* err;
-  int64_t records;            // partial records: 128 sums each, then 2 statistics each
+  int64_t records;            // partial records times rows: 128 sums each, then 2 statistics each
   int64_t most;               // tokens a sequence may have: min(max_len, table_pages page)
   pages::Div tiles, group;    // 16-token tiles of a page; heads of a group
   uint32_t pool_pages;
-  int32_t Hkv, Hq, G, B, rows, table_pages, max_nodes, words, chunk, chunks, blocks, bf16;
+  int32_t Hkv, Hq, G, B, rows, table_pages, max_nodes, words, shares, blocks, bf16;
 };
+
+// The kernel's arguments in constant memory, read where they are used: held in scalar registers from the start they
+// would not leave the loop enough of those, and what does not fit takes vector registers.
+typedef const __attribute__((address_space(4))) TreeArgs* ArgPtr;
+__device__ __forceinline__ ArgPtr arguments() {
+  uint64_t p = (uint64_t)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));   // (another read is another value to the compiler)
+  return (ArgPtr)p;
+}
+__device__ __forceinline__ pages::Div group_of(ArgPtr a) { return {a->group.d, a->group.m, a->group.s}; }
+__device__ __forceinline__ pages::Div tiles_of(ArgPtr a) { return {a->tiles.d, a->tiles.m, a->tiles.s}; }
+
+// The thread's number as a new value: what is computed from it stays where it is computed, instead of being carried in
+// registers from the start of the kernel through its loops.
+__device__ __forceinline__ int thread_again() {
+  int t = threadIdx.x;
+  asm volatile("" : "+v"(t));
+  return t;
+}
 
 // Eight codes of a word less their zero-points, as exact fp16: a code in bits 0-3 of a half under the exponent of
 // 1024, one in bits 4-7 under that of 64; then the base, 1024 or 64 plus the zero-point, is subtracted.  Element e is
 // nibble kNib[e].
 constexpr int kNib[8] = {0, 4, 1, 5, 2, 6, 3, 7};
-__device__ __forceinline__ v8h unpack(uint32_t w, v2h b0, v2h b1, v2h b2, v2h b3) {
+// Masks and exponents as register values the compiler knows nothing of: with literals it takes an and and an or for each
+// pair of codes, from registers the one instruction that does both.
+struct Bits {
+  uint32_t m0, m1, e10, e6;
+};
+__device__ __forceinline__ Bits code_bits() {
+  Bits k = {0x000F000Fu, 0x00F000F0u, 0x64006400u, 0x54005400u};
+  asm("" : "+s"(k.m0), "+s"(k.m1), "+v"(k.e10), "+v"(k.e6));
+  return k;
+}
+__device__ __forceinline__ v8h unpack(uint32_t w, const Bits& k, v2h b0, v2h b1, v2h b2, v2h b3) {
   const uint32_t w8 = w >> 8;
-  const v2h h0 = __builtin_bit_cast(v2h, (w & 0x000F000Fu) | 0x64006400u) - b0;
-  const v2h h1 = __builtin_bit_cast(v2h, (w & 0x00F000F0u) | 0x54005400u) - b1;
-  const v2h h2 = __builtin_bit_cast(v2h, (w8 & 0x000F000Fu) | 0x64006400u) - b2;
-  const v2h h3 = __builtin_bit_cast(v2h, (w8 & 0x00F000F0u) | 0x54005400u) - b3;
+  const v2h h0 = __builtin_bit_cast(v2h, (w & k.m0) | k.e10) - b0;
+  const v2h h1 = __builtin_bit_cast(v2h, (w & k.m1) | k.e6) - b1;
+  const v2h h2 = __builtin_bit_cast(v2h, (w8 & k.m0) | k.e10) - b2;
+  const v2h h3 = __builtin_bit_cast(v2h, (w8 & k.m1) | k.e6) - b3;
   return v8h{h0[0], h0[1], h1[0], h1[1], h2[0], h2[1], h3[0], h3[1]};
+}
+
+// Largest of three, in one instruction (fmaxf would first quiet each operand); a NaN is passed over
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+// x less one half of a pair of fp16 values, exact here, in one instruction
+__device__ __forceinline__ float less_low(float x, v2h h) {
+  float r;
+  asm("v_fma_mix_f32 %0, -%1, 1.0, %2 op_sel_hi:[1,0,0]" : "=v"(r) : "v"(h), "v"(x));
+  return r;
+}
+__device__ __forceinline__ float less_high(float x, v2h h) {
+  float r;
+  asm("v_fma_mix_f32 %0, -%1, 1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(r) : "v"(h), "v"(x));
+  return r;
 }
 
 // Where a wave's token lies: lane l holds the cache row of token t0 + l, 0 for one that is not there.
@@ -95,7 +141,7 @@ struct Rows {
 // A wave's own staging area, and the area where the waves' sums meet
 struct Stage {
   uint32_t v[kStep * kD / 8];   // value codes, 64 bytes a token, 16-byte pieces of row r at piece ^ (r / 16)
-  float ks[kStep], ls[kStep], rs[kStep];   // key scale; log2 and reciprocal of the value scale
+  float ks[kStep], ls[kStep], rs[kStep];   // key scale log2 e / sqrt(128); log2 and reciprocal of the value scale
   uint32_t kz[kStep];           // 1024 + key zero-point as fp16, twice
   _Float16 vz[kStep];           // 1024 (tokens of odd place in their four: 64) + value zero-point, in the order of use
 };
@@ -111,46 +157,88 @@ __device__ __forceinline__ uint16_t to_bits(float f, int bf16) {
   return (uint16_t)(f == f ? (u + 0x7FFFu + ((u >> 16) & 1u)) >> 16 : (u >> 16) | 0x40u);
 }
 
+__device__ __forceinline__ pages::Seq sequence_of(ArgPtr a, int b) {
+  return pages::sequence(a->starts[b], a->starts[b + 1], a->lens[b], a->rows, a->max_nodes, a->most);
+}
+// The rounds of all sequences before each one (times Hkv: before its first KV head), by the first wave; sequences without
+// nodes have none.
+__device__ __forceinline__ void add_rounds(ArgPtr a, int32_t* before, bool flag) {
+  if (threadIdx.x < 64) {
+    int32_t sum = 0;
+    if (threadIdx.x == 0) before[0] = 0;
+    const int B = a->B;
+    for (int b0 = 0; b0 < B; b0 += 64) {
+      const int b = b0 + (int)threadIdx.x;
+      int32_t r = 0;
+      if (b < B) {
+        const pages::Seq sq = sequence_of(a, b);
+        r = sq.n > 0 ? pages::rounds_of(sq.len) : 0;
+        if (flag && sq.bad) dev::flag_error(a->err, kDevErrIndex);
+      }
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const int32_t up = __shfl_up(r, d);
+        if ((int)threadIdx.x >= d) r += up;
+      }
+      if (b < B) before[b + 1] = sum + r;
+      sum += __shfl(r, 63);
+    }
+  }
+  __syncthreads();
+}
+
+// A run of rounds of one unit for the 16 RT rows from r0 on; whole: the run is all of the unit, so its result is final.
+struct Run {
+  int b, kv, r0;
+  int32_t lo, hi;    // rounds of 256 tokens
+  bool whole;
+  int64_t record;
+};
+
 template <int RT>
-__global__ __launch_bounds__(256) void k_tree(TreeArgs a) {
-  __shared__ __attribute__((aligned(16))) Lds lds;
-  __shared__ float stat[2][kWaves][16 * RT];   // reference, sum of exponentials
-  const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, kg = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // blocks of rows over the same chunk are 8 workgroups apart: one XCD, whose L2 then holds the chunk
-  const uint32_t per = 8u * (uint32_t)a.blocks;
-  const uint32_t unit = (blockIdx.x / per) * 8 + blockIdx.x % 8, block = (blockIdx.x % per) / 8;
-  const uint32_t chunk = unit % (uint32_t)a.chunks, kvb = unit / (uint32_t)a.chunks;
-  const int kv = (int)(kvb % (uint32_t)a.Hkv), b = (int)(kvb / (uint32_t)a.Hkv);
-  if (b >= a.B) return;
-  const pages::Seq sq = pages::sequence(a.starts[b], a.starts[b + 1], a.lens[b], a.rows, a.max_nodes, a.most);
-  if (sq.bad && block == 0 && chunk == 0 && kv == 0 && tid == 0) dev::flag_error(a.err, kDevErrIndex);
-  const int nrows = sq.n * a.G, r0 = (int)block * 16 * RT;
-  if (r0 >= nrows) return;
-  const int32_t end = pages::last_token(sq, a.visible != nullptr, a.group, 16 * RT, (int32_t)block);
-  const int32_t t_lo = (int32_t)chunk * a.chunk;
-  if (t_lo >= end && chunk > 0) return;
-  const int32_t t_hi = end - t_lo < a.chunk ? end : t_lo + a.chunk;
+struct Tree {
+  Lds lds;
+  float stat[2][kWaves][16 * RT];   // reference, sum of exponentials
+};
+
+template <int RT>
+__device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, const Run& run) {
+  const int lane = thread_again() & 63, c = lane & 15, kg = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int b = run.b, kv = run.kv, r0 = run.r0;
+  Lds& lds = sh.lds;
+  auto& stat = sh.stat;
+  const int32_t t_lo = run.lo * kRound;
+  int32_t t_hi = run.hi * kRound;
 
   // ---- the queries: B operands, element e of step st is dimension 32 kg + 8 st + kNib[e] of row c
   v8h qb[RT][4];
-  float rowf[RT];      // a row's scores as powers of two: raw score times this
+  float rowf[RT];      // bf16 rows brought into fp16's range by a power of two: the factor that takes it back
+  bool ranged = false; // whether any row is one
   int32_t node[RT];
+  {
+  const ArgPtr a = arguments();
+  const pages::Div group = group_of(a);
+  const int G = a->G, nrows = sq.n * G;
+  const uint16_t* q = a->q;
+  const int64_t stride = a->q_stride;
+  const int32_t end = pages::last_token(sq, a->visible != nullptr, group, 16 * RT, r0 / (16 * RT));
+  if (end < t_hi) t_hi = end;
+  const bool bf16 = a->bf16 != 0;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const int r = r0 + 16 * rt + c;
     const bool in = r < nrows;
     const int rr = in ? r : nrows - 1;
-    node[rt] = (int32_t)pages::quotient((uint32_t)rr, a.group);
-    const int h = kv * a.G + rr - node[rt] * a.G;
-    const uint4* src = reinterpret_cast<const uint4*>(a.q + (int64_t)(sq.row0 + node[rt]) * a.q_stride + (int64_t)h * kD + 32 * kg);
-    constexpr float unit_score = 0.088388347648318447f * 1.4426950408889634f;   // 1 / sqrt(128), log2 e
+    node[rt] = (int32_t)pages::quotient((uint32_t)rr, group);
+    const int h = kv * G + rr - node[rt] * G;
+    const uint4* src = reinterpret_cast<const uint4*>(q + (int64_t)(sq.row0 + node[rt]) * stride + (int64_t)h * kD + 32 * kg);
     uint4 u[4];
 #pragma unroll
     for (int st = 0; st < 4; ++st) u[st] = in ? src[st] : make_uint4(0, 0, 0, 0);
-    if (a.bf16) {
-      // scaled by a power of two that brings the row's largest into [2^14, 2^15): 8 significant bits stay exact in
-      // fp16 down to 2^-28 of it
+    if (bf16) {
+      // 8 significant bits are exact in fp16 from 2^-17 to 2^16 (and off by 2^-25 at most below): a row whose largest is
+      // outside [2^-4, 2^15) is scaled by a power of two that brings it to [2^14, 2^15)
       float top = 0.f;
 #pragma unroll
       for (int st = 0; st < 4; ++st) {
@@ -160,8 +248,9 @@ __global__ __launch_bounds__(256) void k_tree(TreeArgs a) {
       }
       top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32));
-      const int ex = top > 0.f && top < INFINITY ? 14 - ilogbf(top) : 0;
-      rowf[rt] = ldexpf(unit_score, -ex);
+      const int ex = top > 0.f && top < INFINITY && !(top >= 0x1p-4f && top < 0x1p15f) ? 14 - ilogbf(top) : 0;
+      rowf[rt] = ldexpf(1.f, -ex);
+      ranged |= __any(ex != 0);
 #pragma unroll
       for (int st = 0; st < 4; ++st) {
         const uint32_t w[4] = {u[st].x, u[st].y, u[st].z, u[st].w};
@@ -172,7 +261,7 @@ __global__ __launch_bounds__(256) void k_tree(TreeArgs a) {
         }
       }
     } else {
-      rowf[rt] = unit_score;
+      rowf[rt] = 1.f;
 #pragma unroll
       for (int st = 0; st < 4; ++st) {
         const v8h x = __builtin_bit_cast(v8h, u[st]);
@@ -180,6 +269,7 @@ __global__ __launch_bounds__(256) void k_tree(TreeArgs a) {
         for (int e = 0; e < 8; ++e) qb[rt][st][e] = x[kNib[e]];
       }
     }
+  }
   }
 
   float m[RT], l[RT];
@@ -191,52 +281,52 @@ __global__ __launch_bounds__(256) void k_tree(TreeArgs a) {
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) o[rt][dt] = v4f{0.f, 0.f, 0.f, 0.f};
   }
+  const Bits bits = code_bits();
   bool direct = false;         // the sum of exponentials is taken of the scores, not of the weights
   Stage& sg = lds.stage[wave];
-  const int32_t* table = a.table + (int64_t)b * a.table_pages;
+  const ArgPtr a = arguments();
+  const int32_t* table = a->table + (int64_t)b * a->table_pages;
+  const uint8_t *kc = a->kc, *kz = a->kz, *vc = a->vc, *vz = a->vz;
+  const float *ks = a->ks, *vs = a->vs;
+  const pages::Div tiles = tiles_of(a);
+  const uint32_t pool_pages = a->pool_pages, Hkv = (uint32_t)a->Hkv;
   auto entry = [&](int32_t t0) {   // the table's entry of token t0 + lane (anything for a token that is not there)
     const int32_t t = t0 + lane;
-    return table[t < t_hi ? pages::table_index((uint32_t)t, a.tiles) : 0u];
+    return table[t < t_hi ? pages::table_index((uint32_t)t, tiles) : 0u];
   };
+  bool bad = false;            // a table entry that names no page
   auto rows_of = [&](int32_t t0, int32_t e) {
     const int32_t t = t0 + lane;
     Rows r;
-    r.ok = t < t_hi && (uint32_t)e < a.pool_pages;
-    if (t < t_hi && !r.ok) dev::flag_error(a.err, kDevErrIndex);
-    r.row = r.ok ? pages::token_row((uint32_t)t, (uint32_t)e, (uint32_t)a.Hkv, (uint32_t)kv, a.tiles) : 0u;
+    r.ok = t < t_hi && (uint32_t)e < pool_pages;
+    bad |= t < t_hi && !r.ok;
+    r.row = r.ok ? pages::token_row((uint32_t)t, (uint32_t)e, Hkv, (uint32_t)kv, tiles) : 0u;
     return r;
   };
-  // 16 tokens from row `first` on (a page holds whole tiles of 16, so all of them are rows of the cache)
-  auto load_tile = [&](const uint8_t* codes, uint32_t first, int token, int piece) {
-    return *reinterpret_cast<const uint4*>(codes + (uint64_t)(first + (uint32_t)token) * (kD / 2) + 16 * piece);
+  // A step's loads.  Its value codes, scales and zero-points go to LDS when it begins, its key codes are used from
+  // registers; the next step's are sent once they are, without a branch (a step past the end reads the cache's first
+  // rows).  A tile of 16 tokens is 1 KB from its first row on (a page holds whole tiles): a uniform address and a fixed
+  // offset of the lane.
+  uint4 vw[4], kw[4];
+  float ksl, vsl;
+  uint32_t kzl, vzl;
+  Rows cur;
+  int32_t ahead;               // the next step's table entry
+  const uint32_t koff = 64u * (uint32_t)c + 16u * (uint32_t)kg, voff = 16u * (uint32_t)lane;
+  auto load = [&](const Rows& r) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint64_t first = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)r.row, 16 * j) * (kD / 2);
+      vw[j] = *reinterpret_cast<const uint4*>(vc + first + voff);
+      kw[j] = *reinterpret_cast<const uint4*>(kc + first + koff);
+    }
+    ksl = ks[r.row];
+    vsl = vs[r.row];
+    kzl = kz[r.row];
+    vzl = vz[r.row];
   };
 
-  int32_t t0 = t_lo + wave * kStep;
-  uint4 kw[4], vw[4];
-  float ksl = 0.f, vsl = 0.f;
-  uint32_t kzl = 0, vzl = 0;
-  Rows cur{0, false};
-  int32_t ahead = 0;           // the next step's table entry
-  if (t0 < t_hi) {
-    cur = rows_of(t0, entry(t0));
-    ahead = entry(t0 + kRound);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint32_t first = (uint32_t)__builtin_amdgcn_readlane((int)cur.row, 16 * j);
-      vw[j] = load_tile(a.vc, first, lane >> 2, lane & 3);
-    }
-    ksl = a.ks[cur.row];
-    vsl = a.vs[cur.row];
-    kzl = a.kz[cur.row];
-    vzl = a.vz[cur.row];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint32_t first = (uint32_t)__builtin_amdgcn_readlane((int)cur.row, 16 * j);
-      kw[j] = load_tile(a.kc, first, c, kg);
-    }
-  }
-
-  for (; t0 < t_hi; t0 += kRound) {
+  auto step = [&](int32_t t0) {
     const uint64_t there = __ballot(cur.ok);
     // ---- stage the step's scales, zero-points and value codes (a wave's LDS operations keep their order)
     {
@@ -254,12 +344,11 @@ __global__ __launch_bounds__(256) void k_tree(TreeArgs a) {
         if (zero) v = kLeast;
         direct |= __any(cur.ok && (zero || far));
       }
-      sg.ks[lane] = ksl;
+      sg.ks[lane] = ksl * (0.088388347648318447f * 1.4426950408889634f);   // 1 / sqrt(128), log2 e
       sg.ls[lane] = __builtin_amdgcn_logf(v);
       sg.rs[lane] = cur.ok && !direct && vsl < INFINITY ? __builtin_amdgcn_rcpf(v) : 0.f;   // (NaN: w is NaN where it is seen)
-      const _Float16 kb = (_Float16)(1024.f + (float)kzl);
-      const v2h kb2 = {kb, kb};
-      sg.kz[lane] = __builtin_bit_cast(uint32_t, kb2);
+      const _Float16 kzb = (_Float16)(1024.f + (float)kzl);
+      sg.kz[lane] = __builtin_bit_cast(uint32_t, v2h{kzb, kzb});
       // token 16 j + 4 g + i goes to pair i of half j / 2 of lane group g, element j mod 2
       const int tj = lane >> 4, tg = (lane >> 2) & 3, ti = lane & 3;
       sg.vz[tg * 16 + (tj >> 1) * 8 + ti * 2 + (tj & 1)] = (_Float16)((ti & 1 ? 64.f : 1024.f) + (float)vzl);
@@ -269,132 +358,131 @@ __global__ __launch_bounds__(256) void k_tree(TreeArgs a) {
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    // ---- the next step's loads, its key codes after this step's are used
-    const int32_t tn = t0 + kRound;
-    Rows nxt{0, false};
-    if (tn < t_hi) {
-      nxt = rows_of(tn, ahead);
-      ahead = entry(tn + kRound);
+    // ---- scores, at once as powers of two with the value's scale: y = score + log2 s of token 16 j + 4 kg + i.  Four
+    // independent sums at a time: 4 / RT tiles of tokens.
+    v4f y[RT][4];
+    constexpr int TJ = 4 / RT;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t first = (uint32_t)__builtin_amdgcn_readlane((int)nxt.row, 16 * j);
-        vw[j] = load_tile(a.vc, first, lane >> 2, lane & 3);
-      }
-      ksl = a.ks[nxt.row];
-      vsl = a.vs[nxt.row];
-      kzl = a.kz[nxt.row];
-      vzl = a.vz[nxt.row];
-    }
-    // ---- scores
-    v4f sc[RT][4];
+    for (int j0 = 0; j0 < 4; j0 += TJ) {
+      v2h b10[TJ], b6[TJ];
+      v4f acc[TJ][RT];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const v2h b10 = __builtin_bit_cast(v2h, sg.kz[16 * j + c]);
-      const v2h b6 = b10 - v2h{(_Float16)960.f, (_Float16)960.f};
-      const uint32_t w[4] = {kw[j].x, kw[j].y, kw[j].z, kw[j].w};
-      v8h ka[4];
+      for (int j = 0; j < TJ; ++j) {
+        b10[j] = __builtin_bit_cast(v2h, sg.kz[16 * (j0 + j) + c]);
+        b6[j] = b10[j] - v2h{(_Float16)960.f, (_Float16)960.f};
 #pragma unroll
-      for (int st = 0; st < 4; ++st) ka[st] = unpack(w[st], b10, b6, b10, b6);
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        v4f acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int st = 0; st < 4; ++st) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(ka[st], qb[rt][st], acc, 0, 0, 0);
-        sc[rt][j] = acc;
-      }
-    }
-    if (tn < t_hi) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t first = (uint32_t)__builtin_amdgcn_readlane((int)nxt.row, 16 * j);
-        kw[j] = load_tile(a.kc, first, c, kg);
-      }
-    }
-    // ---- softmax: weights p s as two fp16 parts, B operands of the value phase
-    v8h ahi[RT][2], alo[RT][2];
-    auto softmax = [&](auto masked) {
-      constexpr bool kMasked = decltype(masked)::value;
-      v4f k4[4], l4[4], r4[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        k4[j] = *reinterpret_cast<const v4f*>(&sg.ks[16 * j + 4 * kg]);
-        l4[j] = *reinterpret_cast<const v4f*>(&sg.ls[16 * j + 4 * kg]);
-        r4[j] = *reinterpret_cast<const v4f*>(&sg.rs[16 * j + 4 * kg]);
+        for (int rt = 0; rt < RT; ++rt) acc[j][rt] = v4f{0.f, 0.f, 0.f, 0.f};
       }
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        uint32_t seen[2] = {0, 0};   // bits 16 (j mod 2) + i of word j / 2: token 16 j + 4 kg + i
-        if constexpr (kMasked) {
-          uint64_t bits;
-          if (a.visible) {
-            const int32_t d0 = t0 - sq.ctx;
-            uint64_t w0 = 0, w1 = 0;
-            const int32_t k0 = d0 > 0 ? d0 >> 6 : 0;
-            if (d0 > -64) {
-              const uint64_t* row = a.visible + (int64_t)(sq.row0 + node[rt]) * a.words;
-              if (k0 < a.words) w0 = row[k0];
-              if (k0 + 1 < a.words) w1 = row[k0 + 1];
-            }
-            bits = pages::tree_bits(d0, w0, w1);
-          } else {
-            bits = pages::chain_bits(t0, sq.ctx, node[rt]);
-          }
-          bits = (bits & there) >> (4 * kg);
-          seen[0] = (uint32_t)bits;
-          seen[1] = (uint32_t)(bits >> 32);
+      for (int st = 0; st < 4; ++st)
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) {
+          const uint4& u = kw[j0 + j];
+          const v8h kd = unpack(st == 0 ? u.x : st == 1 ? u.y : st == 2 ? u.z : u.w, bits, b10[j], b6[j], b10[j], b6[j]);
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) acc[j][rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kd, qb[rt][st], acc[j][rt], 0, 0, 0);
         }
-        float y[16], top = -INFINITY;
+      if (ranged) {
+#pragma unroll
+        for (int j = 0; j < TJ; ++j)
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) acc[j][rt] *= rowf[rt];
+      }
+#pragma unroll
+      for (int j = 0; j < TJ; ++j) {
+        const v4f k4 = *reinterpret_cast<const v4f*>(&sg.ks[16 * (j0 + j) + 4 * kg]);
+        const v4f l4 = *reinterpret_cast<const v4f*>(&sg.ls[16 * (j0 + j) + 4 * kg]);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) y[rt][j0 + j][i] = fmaf(acc[j][rt][i], k4[i], l4[i]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    // ---- the next step's loads
+    const Rows nxt = rows_of(t0 + kRound, ahead);
+    ahead = entry(t0 + 2 * kRound);
+    load(nxt);
+    __builtin_amdgcn_sched_barrier(0);
+    // ---- what a row does not see
+    if (there != ~uint64_t(0) || t0 + kStep > sq.ctx) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        uint64_t see;
+        const ArgPtr a = arguments();
+        const uint64_t* visible = a->visible;
+        const int32_t words = a->words;
+        if (visible) {
+          const int32_t d0 = t0 - sq.ctx;
+          uint64_t w0 = 0, w1 = 0;
+          const int32_t k0 = d0 > 0 ? d0 >> 6 : 0;
+          if (d0 > -64) {
+            const uint64_t* row = visible + (int64_t)(sq.row0 + node[rt]) * words;
+            if (k0 < words) w0 = row[k0];
+            if (k0 + 1 < words) w1 = row[k0 + 1];
+          }
+          see = pages::tree_bits(d0, w0, w1);
+        } else {
+          see = pages::chain_bits(t0, sq.ctx, node[rt]);
+        }
+        see = (see & there) >> (4 * kg);   // bit 16 j + i: token 16 j + 4 kg + i
+        const uint32_t seen[2] = {(uint32_t)see, (uint32_t)(see >> 32)};
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float v = fmaf(sc[rt][j][i] * k4[j][i], rowf[rt], l4[j][i]);
-            if constexpr (kMasked) v = (seen[j >> 1] >> (16 * (j & 1) + i)) & 1u ? v : -INFINITY;
-            y[4 * j + i] = v;
-          }
-#pragma unroll
-        for (int e = 0; e < 16; ++e) top = fmaxf(top, y[e]);
-        if (__any(top > m[rt] + (kTop + kSlack))) {
-          top = fmaxf(top, __shfl_xor(top, 16));
-          top = fmaxf(top, __shfl_xor(top, 32));
-          const float mn = fmaxf(m[rt], top - kTop), f = __builtin_amdgcn_exp2f(m[rt] - mn);
-          l[rt] = scaled(l[rt], m[rt] - mn);
-          m[rt] = mn;
-#pragma unroll
-          for (int dt = 0; dt < 8; ++dt) o[rt][dt] *= f;
-        }
-        float w[16];
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          w[e] = __builtin_amdgcn_exp2f(y[e] - m[rt]);
-          l[rt] = fmaf(w[e], r4[e >> 2][e & 3], l[rt]);
-        }
-        if constexpr (kMasked) {
-          if (direct) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const float d = fmaf(sc[rt][e >> 2][e & 3] * k4[e >> 2][e & 3], rowf[rt], -m[rt]);
-              l[rt] += (seen[e >> 3] >> (16 * ((e >> 2) & 1) + (e & 3))) & 1u ? __builtin_amdgcn_exp2f(d) : 0.f;
-            }
-          }
-        }
-        // half h, pair i: tokens 16 (2 h) + 4 kg + i and 16 (2 h + 1) + 4 kg + i
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float x = w[8 * h + i], z = w[8 * h + 4 + i];
-            const v2h hi = __builtin_bit_cast(v2h, __builtin_amdgcn_cvt_pkrtz(x, z));
-            const v2h lo = __builtin_bit_cast(v2h, __builtin_amdgcn_cvt_pkrtz(x - (float)hi[0], z - (float)hi[1]));
-            ahi[rt][h][2 * i] = hi[0];
-            ahi[rt][h][2 * i + 1] = hi[1];
-            alo[rt][h][2 * i] = lo[0];
-            alo[rt][h][2 * i + 1] = lo[1];
-          }
+          for (int i = 0; i < 4; ++i) y[rt][j][i] = (seen[j >> 1] >> (16 * (j & 1) + i)) & 1u ? y[rt][j][i] : -INFINITY;
       }
-    };
-    if (direct || there != ~uint64_t(0) || t0 + kStep > sq.ctx) softmax(std::integral_constant<bool, true>{});
-    else softmax(std::integral_constant<bool, false>{});
+    }
+    // ---- softmax: weights w as two fp16 parts, B operands of the value phase
+    v8h ahi[RT][2], alo[RT][2];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) top = max3(max3(top, y[rt][j][0], y[rt][j][1]), y[rt][j][2], y[rt][j][3]);
+      if (__any(top > m[rt] + (kTop + kSlack))) {
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float mn = fmaxf(m[rt], top - kTop), f = __builtin_amdgcn_exp2f(m[rt] - mn);
+        l[rt] = scaled(l[rt], m[rt] - mn);
+        m[rt] = mn;
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) o[rt][dt] *= f;
+      }
+    }
+    if (direct) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const v4f l4 = *reinterpret_cast<const v4f*>(&sg.ls[16 * j + 4 * kg]);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            l[rt] += y[rt][j][i] > -INFINITY ? __builtin_amdgcn_exp2f(y[rt][j][i] - l4[i] - m[rt]) : 0.f;
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      // half h, pair i: tokens 16 (2 h) + 4 kg + i and 16 (2 h + 1) + 4 kg + i
+      const v4f r0 = *reinterpret_cast<const v4f*>(&sg.rs[32 * h + 4 * kg]);
+      const v4f r1 = *reinterpret_cast<const v4f*>(&sg.rs[32 * h + 16 + 4 * kg]);
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float x = __builtin_amdgcn_exp2f(y[rt][2 * h][i] - m[rt]), z = __builtin_amdgcn_exp2f(y[rt][2 * h + 1][i] - m[rt]);
+          l[rt] = fmaf(x, r0[i], l[rt]);
+          l[rt] = fmaf(z, r1[i], l[rt]);
+          const v2h hi = __builtin_bit_cast(v2h, __builtin_amdgcn_cvt_pkrtz(x, z));
+          const v2h lo = __builtin_bit_cast(v2h, __builtin_amdgcn_cvt_pkrtz(less_low(x, hi), less_high(z, hi)));
+          ahi[rt][h][2 * i] = hi[0];
+          ahi[rt][h][2 * i + 1] = hi[1];
+          alo[rt][h][2 * i] = lo[0];
+          alo[rt][h][2 * i + 1] = lo[1];
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
     // ---- values: A = 16 dimensions x 32 tokens of code - z.  The transposing read hands lane (c, kg) the 16 codes of
     // dimension 16 dt + c whose rows the 16 lanes of its group name: token 16 (c / 4) + 4 kg + c mod 4, nibble c.
     {
@@ -409,45 +497,68 @@ __global__ __launch_bounds__(256) void k_tree(TreeArgs a) {
         bz[h][3] = __builtin_bit_cast(v2h, z.w);
       }
       const int row = 16 * (c >> 2) + 4 * kg + (c & 3);
+      constexpr int TD = 4 / RT;   // dimension tiles at a time, for four independent sums
 #pragma unroll
-      for (int dt = 0; dt < 8; ++dt) {
-        const int off = row * (kD / 8) + 4 * ((dt >> 1) ^ (c >> 2)) + 2 * (dt & 1);
-        const v2i t = __builtin_amdgcn_ds_read_tr4_b64_v2i32((__attribute__((address_space(3))) v2i*)(sg.v + off));
+      for (int d0 = 0; d0 < 8; d0 += TD) {
+        v2i t[TD];
+#pragma unroll
+        for (int d = 0; d < TD; ++d) {
+          const int dt = d0 + d, off = row * (kD / 8) + 4 * ((dt >> 1) ^ (c >> 2)) + 2 * (dt & 1);
+          t[d] = __builtin_amdgcn_ds_read_tr4_b64_v2i32((__attribute__((address_space(3))) v2i*)(sg.v + off));
+        }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const v8h va = unpack(h ? (uint32_t)t.y : (uint32_t)t.x, bz[h][0], bz[h][1], bz[h][2], bz[h][3]);
+          v8h va[TD];
 #pragma unroll
-          for (int rt = 0; rt < RT; ++rt) {
-            o[rt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va, ahi[rt][h], o[rt][dt], 0, 0, 0);
-            o[rt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va, alo[rt][h], o[rt][dt], 0, 0, 0);
-          }
+          for (int d = 0; d < TD; ++d) va[d] = unpack(h ? (uint32_t)t[d].y : (uint32_t)t[d].x, bits, bz[h][0], bz[h][1], bz[h][2], bz[h][3]);
+#pragma unroll
+          for (int part = 0; part < 2; ++part)
+#pragma unroll
+            for (int d = 0; d < TD; ++d)
+#pragma unroll
+              for (int rt = 0; rt < RT; ++rt)
+                o[rt][d0 + d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va[d], part ? alo[rt][h] : ahi[rt][h], o[rt][d0 + d], 0, 0, 0);
         }
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
     cur = nxt;
+  };
+  int32_t t0 = t_lo + wave * kStep;
+  if (t0 < t_hi) {
+    cur = rows_of(t0, entry(t0));
+    ahead = entry(t0 + kRound);
+    load(cur);
+    for (; t0 < t_hi; t0 += kRound) step(t0);
   }
+
+  const ArgPtr z = arguments();
+  if (bad) dev::flag_error(z->err, kDevErrIndex);
+  const int G = z->G, nrows = sq.n * G;
+  const pages::Div group = group_of(z);
+  const int tid = thread_again(), c2 = tid & 15, kg2 = (tid >> 4) & 3;
 
   // ---- the four waves' sums meet under a common reference
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     l[rt] += __shfl_xor(l[rt], 16);
     l[rt] += __shfl_xor(l[rt], 32);
-    if (kg == 0) {
-      stat[0][wave][16 * rt + c] = m[rt];
-      stat[1][wave][16 * rt + c] = l[rt];
+    if (kg2 == 0) {
+      stat[0][wave][16 * rt + c2] = m[rt];
+      stat[1][wave][16 * rt + c2] = l[rt];
     }
   }
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     __syncthreads();   // the staging areas, or the last tile's sums, are no longer read
-    float M = stat[0][0][16 * rt + c];
+    float M = stat[0][0][16 * rt + c2];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) M = fmaxf(M, stat[0][w][16 * rt + c]);
+    for (int w = 1; w < kWaves; ++w) M = fmaxf(M, stat[0][w][16 * rt + c2]);
     const float f = __builtin_amdgcn_exp2f(m[rt] - M);
 #pragma unroll
-    for (int dt = 0; dt < 8; ++dt) *reinterpret_cast<v4f*>(&lds.sum[wave][c][16 * dt + 4 * kg]) = o[rt][dt] * f;
+    for (int dt = 0; dt < 8; ++dt) *reinterpret_cast<v4f*>(&lds.sum[wave][c2][16 * dt + 4 * kg2]) = o[rt][dt] * f;
     __syncthreads();
     const int row = tid >> 4, d0 = (tid & 15) * 8, r = r0 + 16 * rt + row;
     float Mr = stat[0][0][16 * rt + row], L = 0.f;
@@ -467,57 +578,123 @@ __global__ __launch_bounds__(256) void k_tree(TreeArgs a) {
       s[e + 3] = x[3];
     }
     if (r < nrows) {
-      if (a.chunks == 1) {
-        const int nd = (int)pages::quotient((uint32_t)r, a.group);
+      if (run.whole) {
+        const int nd = (int)pages::quotient((uint32_t)r, group);
         const float inv = L == 0.f ? 0.f : 1.f / L;   // a row that sees nothing: 0
         uint32_t w[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          w[e] = (uint32_t)to_bits(s[2 * e] * inv, a.bf16) | ((uint32_t)to_bits(s[2 * e + 1] * inv, a.bf16) << 16);
-        uint16_t* y = a.out + ((int64_t)(sq.row0 + nd) * a.Hq + kv * a.G + (r - nd * a.G)) * kD + d0;
+          w[e] = (uint32_t)to_bits(s[2 * e] * inv, z->bf16) | ((uint32_t)to_bits(s[2 * e + 1] * inv, z->bf16) << 16);
+        uint16_t* y = z->out + ((int64_t)(sq.row0 + nd) * z->Hq + kv * G + (r - nd * G)) * kD + d0;
         *reinterpret_cast<uint4*>(y) = make_uint4(w[0], w[1], w[2], w[3]);
       } else {
-        const int64_t rec = (((int64_t)b * a.Hkv + kv) * a.chunks + chunk) * ((int64_t)a.max_nodes * a.G) + r;
-        float* y = a.part + rec * kD + d0;
+        const int64_t rec = run.record * ((int64_t)z->max_nodes * G) + r;
+        float* y = z->part + rec * kD + d0;
         *reinterpret_cast<float4*>(y) = make_float4(s[0], s[1], s[2], s[3]);
         *reinterpret_cast<float4*>(y + 4) = make_float4(s[4], s[5], s[6], s[7]);
         if (d0 == 0) {
-          a.part[a.records * kD + 2 * rec] = Mr;
-          a.part[a.records * kD + 2 * rec + 1] = L;
+          z->part[z->records * kD + 2 * rec] = Mr;
+          z->part[z->records * kD + 2 * rec + 1] = L;
         }
       }
     }
   }
 }
 
-// out = sum_c 2^(m_c - M) sums_c / sum_c 2^(m_c - M) l_c over the chunks c of a row's sequence.  32 lanes of four
-// dimensions take a row, or `slices` times 32 lanes share its chunks.
-__global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a, int32_t block_rows, int32_t slices) {
+template <int RT>
+__global__ __launch_bounds__(256, 2) void k_tree(TreeArgs) {
+  __shared__ __attribute__((aligned(16))) Tree<RT> sh;
+  __shared__ int32_t before[pages::kMostShared + 1];
+  const ArgPtr a = arguments();
+  // blocks of rows over the same tokens are 8 workgroups apart: one XCD, whose L2 then holds the tokens
+  const uint32_t per = 8u * (uint32_t)a->blocks;
+  const uint32_t i = (blockIdx.x / per) * 8 + blockIdx.x % 8, block = (blockIdx.x % per) / 8;
+  Run run;
+  run.r0 = (int)block * 16 * RT;
+  if (a->shares == 0) {
+    run.b = (int)(i / (uint32_t)a->Hkv);
+    run.kv = (int)(i % (uint32_t)a->Hkv);
+    if (run.b >= a->B) return;
+    const pages::Seq sq = sequence_of(a, run.b);
+    if (sq.bad && block == 0 && run.kv == 0 && threadIdx.x == 0) dev::flag_error(a->err, kDevErrIndex);
+    if (run.r0 >= sq.n * a->G) return;
+    run.lo = 0;
+    run.hi = pages::rounds_of(sq.len);
+    run.whole = true;
+    run.record = 0;
+    tree_run<RT>(sh, sq, run);
+    return;
+  }
+  if (i >= (uint32_t)a->shares) return;
+  add_rounds(a, before, blockIdx.x == 0);
+  const int64_t W = (int64_t)__builtin_amdgcn_readfirstlane(before[a->B]) * a->Hkv;
+  const int32_t shares = pages::used_shares(W, a->shares);
+  if ((int32_t)i >= shares) return;
+  int64_t pos = pages::first_round(W, shares, (int32_t)i);
+  const int64_t stop = pages::first_round(W, shares, (int32_t)i + 1);
+  // the sequence of the share's first round: the last one with no more rounds before it (one without rounds has as
+  // many before it as the next)
+  int b = 0;
+  for (int b0 = 0; b0 < a->B; b0 += 64) {
+    const int x = b0 + (int)(threadIdx.x & 63);
+    b += __popcll(__ballot(x < a->B && (int64_t)before[x + 1] * a->Hkv <= pos));
+  }
+  b = __builtin_amdgcn_readfirstlane(b);
+  for (; pos < stop; ++b) {
+    const int32_t first = __builtin_amdgcn_readfirstlane(before[b]), n = __builtin_amdgcn_readfirstlane(before[b + 1]) - first;
+    if (n == 0) continue;
+    const pages::Seq sq = sequence_of(a, b);
+    run.b = b;
+    for (run.kv = (int)((pos - (int64_t)first * a->Hkv) / n); run.kv < a->Hkv && pos < stop; ++run.kv) {
+      const int64_t at = (int64_t)first * a->Hkv + (int64_t)run.kv * n;
+      run.lo = (int32_t)(pos - at);
+      run.hi = stop - at < n ? (int32_t)(stop - at) : n;
+      run.whole = run.lo == 0 && run.hi == n;
+      run.record = (int64_t)i + (int64_t)b * a->Hkv + run.kv;
+      if (run.r0 < sq.n * a->G) {
+        tree_run<RT>(sh, sq, run);
+        __syncthreads();
+      }
+      pos = at + run.hi;
+    }
+  }
+}
+
+// out = sum_i 2^(m_i - M) sums_i / sum_i 2^(m_i - M) l_i over the shares i that cover a row's unit, where there are more
+// than one.  32 lanes of four dimensions take a row, or `slices` times 32 lanes share its records.
+__global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a, int32_t slices) {
+  __shared__ int32_t before[pages::kMostShared + 1];
   __shared__ v4f sum[8][32];
+  const ArgPtr p = arguments();
   const int lane = threadIdx.x & 31, slot = threadIdx.x >> 5;
   const int kv = blockIdx.y, b = blockIdx.z;
-  const pages::Seq sq = pages::sequence(a.starts[b], a.starts[b + 1], a.lens[b], a.rows, a.max_nodes, a.most);
+  const pages::Seq sq = sequence_of(p, b);
   const int nrows = sq.n * a.G, first = (int)blockIdx.x * (8 / slices);
   if (first >= nrows) return;
+  add_rounds(p, before, false);
+  const int64_t W = (int64_t)__builtin_amdgcn_readfirstlane(before[a.B]) * a.Hkv;
+  const int32_t n = before[b + 1] - before[b];
+  const int64_t at = (int64_t)before[b] * a.Hkv + (int64_t)kv * n;
+  const int32_t shares = pages::used_shares(W, a.shares);
+  const int32_t i0 = pages::share_of(W, shares, at), count = pages::share_of(W, shares, at + n - 1) - i0 + 1;
+  if (count == 1) return;
   const int r = first + slot / slices, slice = slot % slices;
   const bool in = r < nrows;
   v4f acc = {0.f, 0.f, 0.f, 0.f};
   float L = 0.f;
   if (in) {
-    const int32_t end = pages::last_token(sq, a.visible != nullptr, a.group, block_rows, r / block_rows);
-    const int32_t n = (end + a.chunk - 1) / a.chunk;
-    const int64_t R = (int64_t)a.max_nodes * a.G, rec = ((int64_t)b * a.Hkv + kv) * a.chunks * R + r;
+    const int64_t R = (int64_t)a.max_nodes * a.G, rec = (i0 + (int64_t)b * a.Hkv + kv) * R + r;
     const float* st = a.part + a.records * kD + 2 * rec;
     float M = kLowest;
-    for (int32_t i = lane; i < n; i += 32) M = fmaxf(M, st[2 * R * i]);
+    for (int32_t i = lane; i < count; i += 32) M = fmaxf(M, st[2 * R * i]);
 #pragma unroll
     for (int d = 16; d; d >>= 1) M = fmaxf(M, __shfl_xor(M, d));
-    for (int32_t i = lane; i < n; i += 32) L += scaled(st[2 * R * i + 1], st[2 * R * i] - M);
+    for (int32_t i = lane; i < count; i += 32) L += scaled(st[2 * R * i + 1], st[2 * R * i] - M);
 #pragma unroll
     for (int d = 16; d; d >>= 1) L += __shfl_xor(L, d);
     const float* y = a.part + rec * kD + 4 * lane;
 #pragma unroll 4
-    for (int32_t i = slice; i < n; i += slices) {
+    for (int32_t i = slice; i < count; i += slices) {
       const float f = __builtin_amdgcn_exp2f(st[2 * R * i] - M);
       acc += *reinterpret_cast<const v4f*>(y + R * kD * i) * f;
     }
@@ -559,7 +736,7 @@ hipError_t launch_kv4_tree(const TreeCall& t, hipStream_t s) {
   a.out = t.out;
   a.part = t.ws;
   a.err = device_error_word();
-  a.records = pages::records(p, t.B, c.Hkv, G, t.max_nodes);
+  a.records = pages::records(p, t.B, c.Hkv) * ((int64_t)t.max_nodes * G);
   const int64_t room = (int64_t)t.table_pages * c.page;
   a.most = t.max_len < room ? t.max_len : room;
   a.tiles = pages::make_div((uint32_t)c.page / 16);
@@ -573,21 +750,21 @@ hipError_t launch_kv4_tree(const TreeCall& t, hipStream_t s) {
   a.table_pages = t.table_pages;
   a.max_nodes = t.max_nodes;
   a.words = (t.max_nodes + 63) / 64;
-  a.chunk = p.chunk;
-  a.chunks = p.chunks;
+  a.shares = p.shares;
   a.blocks = p.blocks;
   a.bf16 = t.dtype == kBF16;
-  const int64_t units = (t.B * c.Hkv * p.chunks + 7) / 8 * 8;
+  const int64_t units = ((p.shares ? p.shares : t.B * c.Hkv) + 7) / 8 * 8;
   const dim3 grid((unsigned)(units * p.blocks));
   auto kernel = p.rt == 1 ? k_tree<1> : k_tree<2>;
   hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.chunks == 1) return e;
-  // rows of many chunks are shared by 8 slices, of few by 2
-  const int32_t slices = p.chunks > 16 ? 8 : p.chunks > 4 ? 4 : 2;
+  if (e != hipSuccess || p.shares == 0) return e;
+  // the records of a row: about as many as shares to a unit, and one more; many are shared by 8 slices
+  const int64_t each = p.shares / (t.B * c.Hkv) + 2;
+  const int32_t slices = each > 16 ? 8 : each > 4 ? 4 : 2;
   const int64_t R = (int64_t)t.max_nodes * G;
   const dim3 mgrid((unsigned)((R * slices + 7) / 8), (unsigned)c.Hkv, (unsigned)t.B);
-  hipLaunchKernelGGL(k_tree_merge, mgrid, dim3(256), 0, s, a, 16 * p.rt, slices);
+  hipLaunchKernelGGL(k_tree_merge, mgrid, dim3(256), 0, s, a, slices);
   return hipGetLastError();
 }
 

@@ -63,7 +63,15 @@ int main() {
       long long B, len; int Hkv, G, nodes;
       std::scanf("%lld %d %d %d %lld", &B, &Hkv, &G, &nodes, &len);
       const Plan p = plan(B, Hkv, G, nodes, len);
-      std::printf("%d %d %d %d %lld\n", p.rt, p.blocks, p.chunk, p.chunks, (long long)records(p, B, Hkv, G, nodes));
+      std::printf("%d %d %d %lld\n", p.rt, p.blocks, p.shares, (long long)records(p, B, Hkv));
+    } else if (!std::strcmp(what, "used")) {
+      long long W; int n;
+      std::scanf("%lld %d", &W, &n);
+      std::printf("%d\n", used_shares(W, n));
+    } else if (!std::strcmp(what, "share")) {
+      long long W, r; int n, i;
+      std::scanf("%lld %d %d %lld", &W, &n, &i, &r);
+      std::printf("%lld %lld %d\n", (long long)first_round(W, n, i), (long long)first_round(W, n, i + 1), share_of(W, n, r));
     }
   }
 }
@@ -174,16 +182,48 @@ def test_last_token_of_a_block_of_rows(ask):
     assert [g[0] for g in ask(lines)] == want
 
 
-def test_plan_covers_every_row_and_token(ask):
+def test_plan_covers_every_row(ask):
     rng = np.random.default_rng(7)
     lines = []
     for _ in range(3000):
         lines.append(("plan", int(np.exp(rng.uniform(0, 11))), int(np.exp(rng.uniform(0, 5))), int(rng.integers(1, 65)),
                       int(rng.integers(1, 257)), int(np.exp(rng.uniform(0, 19.4)))))
-    for (_, B, Hkv, G, nodes, length), (rt, blocks, chunk, chunks, records) in zip(lines, ask(lines)):
+    for (_, B, Hkv, G, nodes, length), (rt, blocks, shares, records) in zip(lines, ask(lines)):
         assert rt in (1, 2, 4) and blocks * 16 * rt >= nodes * G > (blocks - 1) * 16 * rt
-        assert chunk % 256 == 0 and chunk * chunks >= length > chunk * (chunks - 1)
-        assert records == (0 if chunks == 1 else B * Hkv * chunks * nodes * G)
+        assert 0 <= shares <= B * Hkv * -(-length // 256) and (B <= 512 or shares == 0)
+        assert records == (shares + B * Hkv if shares else 0)
+
+
+def test_shares_cover_every_round_once(ask):
+    """The runs of units that the shares take, as the kernel walks them: every round once, the records' numbers
+    different and inside the workspace, and the shares that a unit is joined from those that took part of it."""
+    rng = np.random.default_rng(11)
+    for _ in range(60):
+        B, Hkv = int(rng.integers(1, 9)), int(rng.integers(1, 9))
+        rounds = rng.integers(0, 40, B) * rng.integers(0, 2, B)
+        W = int(rounds.sum()) * Hkv
+        n = int(rng.integers(1, 120))
+        if W == 0:
+            continue
+        asked, n = n, ask([("used", W, n)])[0][0]
+        assert n == min(W, asked)
+        units = [(b * Hkv + kv, int(rounds[:b].sum()) * Hkv + kv * int(rounds[b]), int(rounds[b])) for b in range(B) for kv in range(Hkv)]
+        bounds = [g[:2] for g in ask([("share", W, n, i, 0) for i in range(n)])]
+        assert bounds[0][0] == 0 and all(lo < hi for lo, hi in bounds) and bounds[-1][1] == W and all(a[1] == b[0] for a, b in zip(bounds, bounds[1:]))
+        holds = [g[2] for g in ask([("share", W, n, 0, r) for r in range(W)])]
+        assert all(bounds[holds[r]][0] <= r < bounds[holds[r]][1] for r in range(W))
+        seen, numbers = np.zeros(W, int), set()
+        for u, at, k in units:
+            took = []
+            for i, (lo, hi) in enumerate(bounds):
+                lo, hi = max(lo, at), min(hi, at + k)
+                if lo < hi:
+                    seen[lo:hi] += 1
+                    took.append(i)
+                    assert 0 <= i + u < n + B * Hkv and i + u not in numbers
+                    numbers.add(i + u)
+            assert took == ([] if k == 0 else list(range(holds[at], holds[at + k - 1] + 1))) or k == 0
+        assert (seen == 1).all()
 
 
 # ---- the C ABI ---------------------------------------------------------------------------------------------------
