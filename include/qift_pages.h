@@ -66,7 +66,7 @@ typedef struct {
  *   k_values, v_values   out, nullable (both or none): the values s (q - z) that the cache now
  *              stands for, [n][Hkv][128] in dtype (one rounding from fp32), for the attention of the
  *              prompt that is being written; zeros for a token that is not written.
- *   n = 0 does nothing.  Limits: n < 2^31.
+ *   n = 0 does nothing.  Limits: n < 2^31, n * Hkv < 2^34.
  */
 int qift_kv4_append(const qift_kv4_pages *cache, const void *k, const void *v, int64_t k_stride,
                     int64_t v_stride, int32_t dtype, const int32_t *slots, int64_t n, void *k_values,

@@ -51,6 +51,7 @@ int qift_kv4_append(const qift_kv4_pages* cache, const void* k, const void* v, i
   if (dtype != QIFT_F16 && dtype != QIFT_BF16) return QIFT_ERR_FORMAT;
   const int64_t width = (int64_t)cache->Hkv * 128;
   if (n < 0 || n >= k31 || k_stride < width || v_stride < width || k_stride >= k31 || v_stride >= k31) return QIFT_ERR_SHAPE;
+  if ((n + 15) / 16 * 2 * cache->Hkv >= k31) return QIFT_ERR_SHAPE;   // one workgroup to 16 tokens, a head and a side
   if (n == 0) return QIFT_OK;
   if (!k || !v || !slots || (!k_values) != (!v_values)) return QIFT_ERR_NULL;
   st = check_pointers(cache);

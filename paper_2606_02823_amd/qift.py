@@ -430,10 +430,13 @@ class KV4Pages:
             _dev(c.codes, torch.uint8, rows + (64,), name + ".codes")
             _dev(c.scales, torch.float32, rows, name + ".scales")
             _dev(c.zeros, torch.uint8, rows, name + ".zeros")
-        _same_device(k.codes, (k.scales, k.zeros, v.codes, v.scales, v.zeros))
+        for t in (k.scales, k.zeros, v.codes, v.scales, v.zeros):
+            if t.device != k.codes.device:
+                raise ValueError(f"the cache's tensors are on {k.codes.device} and {t.device}")
         self.k, self.v = k, v
         self.pages, self.Hkv, self.page = rows
         self.device = k.codes.device
+        self.index = k.codes.get_device()
         self.c = KV4PagesC(self.pages, self.page, self.Hkv, 128, 0, k.codes.data_ptr(), k.scales.data_ptr(),
                            k.zeros.data_ptr(), v.codes.data_ptr(), v.scales.data_ptr(), v.zeros.data_ptr())
         self._ref = ctypes.byref(self.c)
@@ -447,12 +450,6 @@ class KV4Pages:
                          torch.zeros(rows, dtype=torch.uint8, device=device)) for _ in range(2)))
 
 
-def _same_device(t, others):
-    for o in others:
-        if o is not None and o.device != t.device:
-            raise ValueError(f"tensors on {t.device} and {o.device}: one call takes one device")
-
-
 def _empty(shape, dtype, device, stream=None) -> torch.Tensor:
     """Memory for a call on `stream`: taken from that stream's pool, so that what is freed here is not reused by
     another stream while the call runs."""
@@ -462,81 +459,91 @@ def _empty(shape, dtype, device, stream=None) -> torch.Tensor:
         return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _rows(t: torch.Tensor, dtype, heads: int, name: str) -> int:
-    """The row stride of a [rows, heads, 128] view whose rows are contiguous (a part of stacked rows, say)."""
+_HALVES = (torch.float16, torch.bfloat16)
+
+
+# The checks of the paged calls, each one expression where all is well (a decode step's append runs 3 us on the GPU):
+# tensors on the cache's device, of the type and shape; what is wrong is said where an expression fails.
+def _on_device(t, index, name):
     if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
         raise TypeError(f"{name} must be a CUDA (HIP) tensor")
-    if t.dtype != dtype:
-        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != 128:
-        raise ValueError(f"{name} must have shape (rows, {heads}, 128), got {tuple(t.shape)}")
-    n, stride = t.shape[0], t.stride()
-    if n and (stride[2] != 1 or (heads > 1 and stride[1] != 128)):
+    if t.get_device() != index:
+        raise ValueError(f"{name} is on {t.device}, the cache on device {index}")
+
+
+def _dense(t, index, dtype, shape, name):
+    if t.__class__ is torch.Tensor and t.get_device() == index and t.dtype is dtype and t.shape == shape and t.is_contiguous():
+        return
+    _on_device(t, index, name)
+    _dev(t, dtype, shape, name)
+
+
+def _rows(t, index, dtype, shape, name) -> int:
+    """The row stride of a [rows, heads, 128] view whose rows are contiguous (a part of stacked rows, say)."""
+    if not (t.__class__ is torch.Tensor and t.get_device() == index and t.dtype is dtype and t.shape == shape):
+        _on_device(t, index, name)
+        if t.dtype != dtype:
+            raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+        if tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    n, heads = shape[0], shape[1]
+    row, head, one = t.stride()
+    if (one != 1 or (head != 128 and heads > 1)) and n:
         raise ValueError(f"{name} must have contiguous rows")
-    return stride[0] if n > 1 else heads * 128
+    return row if n > 1 else heads * 128
 
 
-class _on:
-    """Makes a tensor's device the current one for a call, where it is not already (the kernels are launched on the
-    current device and its current stream)."""
-
-    def __init__(self, device):
-        self.other = None
-        if device.index is not None and device.index != torch.cuda.current_device():
-            self.other = torch.cuda.device(device)
-
-    def __enter__(self):
-        if self.other is not None:
-            self.other.__enter__()
-
-    def __exit__(self, *exc):
-        if self.other is not None:
-            self.other.__exit__(*exc)
+def _run(index, call, args, stream):
+    """The call on its device (kernels are launched on the current device and its current stream)."""
+    if (_raw_device() if _raw_device is not None else torch.cuda.current_device()) == index:
+        return call(*args, _stream(stream))
+    with torch.cuda.device(index):
+        return call(*args, _stream(stream))
 
 
 def kv4_append(cache: KV4Pages, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, values=False, stream=None):
     """Quantize the keys and values of n new tokens (fp16 or bf16 [n, Hkv, 128], row-strided views taken as they
     are) into their slots (int32 [n]; negative: not written).  values=True, or a pair of tensors [n, Hkv, 128] to
     write: returns (k, v) as the cache now stands for them, else None.  A slot may appear once in a call."""
-    dt = k.dtype
-    if dt not in (torch.float16, torch.bfloat16):
+    dt, index = k.dtype, cache.index
+    if dt not in _HALVES:
         raise TypeError(f"k must be torch.float16 or torch.bfloat16, got {dt}")
-    ks, vs = _rows(k, dt, cache.Hkv, "k"), _rows(v, dt, cache.Hkv, "v")
     n = k.shape[0]
-    if v.shape[0] != n:
-        raise ValueError(f"k has {n} rows, v {v.shape[0]}")
-    _dev(slots, torch.int32, (n,), "slots")
-    out = (None, None)
+    shape = (n, cache.Hkv, 128)
+    ks, vs = _rows(k, index, dt, shape, "k"), _rows(v, index, dt, shape, "v")
+    _dense(slots, index, torch.int32, (n,), "slots")
     if values is True:
-        out = tuple(_empty((n, cache.Hkv, 128), dt, k.device, stream) for _ in range(2))
-    elif values is not False and values is not None:
-        out = tuple(values)
-        for t in out:
-            _dev(t, dt, (n, cache.Hkv, 128), "values")
-    _same_device(cache.k.codes, (k, v, slots, *out))
-    with _on(cache.device):
-        st = lib().qift_kv4_append(cache._ref, k.data_ptr(), v.data_ptr(), ks, vs, _DTYPE[dt], slots.data_ptr(), n,
-                                   _ptr(out[0]), _ptr(out[1]), _stream(stream))
-    _check("qift_kv4_append", st)
-    return None if out[0] is None else out
+        ko, vo = _empty(shape, dt, cache.device, stream), _empty(shape, dt, cache.device, stream)
+    elif values is False or values is None:
+        ko = vo = None
+    else:
+        ko, vo = values
+        _dense(ko, index, dt, shape, "values")
+        _dense(vo, index, dt, shape, "values")
+    st = _run(index, lib().qift_kv4_append, (cache._ref, k.data_ptr(), v.data_ptr(), ks, vs, _DTYPE[dt], slots.data_ptr(), n,
+                                             _ptr(ko), _ptr(vo)), stream)
+    if st:
+        _check("qift_kv4_append", st)
+    return None if ko is None else (ko, vo)
 
 
 def kv4_read(cache: KV4Pages, slots: torch.Tensor, dtype=torch.float16, out=None, stream=None):
     """(k, v) [n, Hkv, 128] of the given slots (int32 [n]; negative: zeros) in dtype fp16, bf16 or fp32."""
     if dtype not in _DTYPE:
         raise TypeError(f"dtype must be torch.float16, torch.bfloat16 or torch.float32, got {dtype}")
-    n = slots.numel()
-    _dev(slots, torch.int32, (n,), "slots")
+    n, index = slots.numel(), cache.index
+    _dense(slots, index, torch.int32, (n,), "slots")
+    shape = (n, cache.Hkv, 128)
     if out is None:
-        out = tuple(_empty((n, cache.Hkv, 128), dtype, cache.device, stream) for _ in range(2))
-    for t in out:
-        _dev(t, dtype, (n, cache.Hkv, 128), "out")
-    _same_device(cache.k.codes, (slots, *out))
-    with _on(cache.device):
-        st = lib().qift_kv4_read(cache._ref, slots.data_ptr(), n, _DTYPE[dtype], out[0].data_ptr(), out[1].data_ptr(),
-                                 _stream(stream))
-    _check("qift_kv4_read", st)
-    return out
+        ko, vo = _empty(shape, dtype, cache.device, stream), _empty(shape, dtype, cache.device, stream)
+    else:
+        ko, vo = out
+        _dense(ko, index, dtype, shape, "out")
+        _dense(vo, index, dtype, shape, "out")
+    st = _run(index, lib().qift_kv4_read, (cache._ref, slots.data_ptr(), n, _DTYPE[dtype], ko.data_ptr(), vo.data_ptr()), stream)
+    if st:
+        _check("qift_kv4_read", st)
+    return ko, vo
 
 
 def kv4_attention_tree_workspace(B: int, Hq: int, Hkv: int, max_nodes: int, max_len: int, device="cuda") -> torch.Tensor:
@@ -553,36 +560,33 @@ def kv4_attention_tree(q: torch.Tensor, cache: KV4Pages, table: torch.Tensor, st
     cached tokens (int32 [B]) in the pages table[b] (int32 [B, table_pages]).  visible (int64 [rows,
     ceil(max_nodes / 64)]): bit j of a row says that it sees node j of its sequence; None: nodes up to its own.
     Returns [rows, Hq, 128] in q's type."""
-    dt = q.dtype
-    if dt not in (torch.float16, torch.bfloat16):
+    dt, index = q.dtype, cache.index
+    if dt not in _HALVES:
         raise TypeError(f"q must be torch.float16 or torch.bfloat16, got {dt}")
-    if q.dim() != 3:
-        raise ValueError(f"q must have shape (rows, Hq, 128), got {tuple(q.shape)}")
-    rows, Hq = q.shape[0], q.shape[1]
-    qs = _rows(q, dt, Hq, "q")
-    if not isinstance(table, torch.Tensor) or table.dim() != 2:
-        raise ValueError("table must have shape (B, table_pages)")
-    B = table.shape[0]
-    _dev(table, torch.int32, (B, table.shape[1]), "table")
-    _dev(starts, torch.int32, (B + 1,), "starts")
-    _dev(lens, torch.int32, (B,), "lens")
+    if q.dim() != 3 or table.dim() != 2:
+        raise ValueError(f"q must have shape (rows, Hq, 128), table (B, table_pages); got {tuple(q.shape)}, {tuple(table.shape)}")
+    rows, Hq, _ = shape = q.shape
+    B, pages = table.shape
+    qs = _rows(q, index, dt, (rows, Hq, 128), "q")
+    _dense(table, index, torch.int32, (B, pages), "table")
+    _dense(starts, index, torch.int32, (B + 1,), "starts")
+    _dense(lens, index, torch.int32, (B,), "lens")
     if visible is not None:
-        _dev(visible, torch.int64, (rows, (max_nodes + 63) // 64), "visible")
+        _dense(visible, index, torch.int64, (rows, (max_nodes + 63) // 64), "visible")
     if out is None:
-        out = _empty((rows, Hq, 128), dt, q.device, stream)
-    _dev(out, dt, (rows, Hq, 128), "out")
+        out = _empty(shape, dt, cache.device, stream)
+    else:
+        _dense(out, index, dt, shape, "out")
     if workspace is None:
         need = int(lib().qift_kv4_attention_tree_workspace_bytes(B, Hq, cache.Hkv, 128, max_nodes, max_len))
-        workspace = _empty(max(need, 16), torch.uint8, q.device, stream)
+        workspace = _empty((max(need, 16),), torch.uint8, cache.device, stream)
     else:
-        _dev(workspace, torch.uint8, (workspace.numel(),), "workspace")
-    _same_device(cache.k.codes, (q, table, starts, lens, visible, out, workspace))
-    with _on(cache.device):
-        st = lib().qift_kv4_attention_tree(cache._ref, q.data_ptr(), qs, _DTYPE[dt], rows, table.data_ptr(),
-                                           table.shape[1], starts.data_ptr(), lens.data_ptr(), B, Hq, max_nodes, max_len,
-                                           _ptr(visible), out.data_ptr(), workspace.data_ptr(), workspace.numel(),
-                                           _stream(stream))
-    _check("qift_kv4_attention_tree", st)
+        _dense(workspace, index, torch.uint8, (workspace.numel(),), "workspace")
+    st = _run(index, lib().qift_kv4_attention_tree,
+              (cache._ref, q.data_ptr(), qs, _DTYPE[dt], rows, table.data_ptr(), pages, starts.data_ptr(), lens.data_ptr(), B,
+               Hq, max_nodes, max_len, _ptr(visible), out.data_ptr(), workspace.data_ptr(), workspace.numel()), stream)
+    if st:
+        _check("qift_kv4_attention_tree", st)
     return out
 
 

@@ -263,7 +263,8 @@ def test_append_refusals(L):
     for bad in BAD_POOLS:
         assert f(cache=pool(**bad)) == E_SHAPE, bad
     assert f(dt=2) == E_FORMAT and f(dt=-1) == E_FORMAT
-    for kw in (dict(n=-1), dict(n=2 ** 31), dict(ks=1023), dict(vs=0), dict(ks=-1024), dict(vs=2 ** 31)):
+    for kw in (dict(n=-1), dict(n=2 ** 31), dict(ks=1023), dict(vs=0), dict(ks=-1024), dict(vs=2 ** 31),
+               dict(cache=pool(pages=1, page=16, Hkv=65535), n=2 ** 20, ks=65535 * 128, vs=65535 * 128)):
         assert f(**kw) == E_SHAPE, kw
     for kw in (dict(k=None), dict(v=None), dict(slots=None), dict(kv=A), dict(vv=A), dict(cache=pool(v_zeros=None))):
         assert f(**kw) == E_NULL, kw
@@ -324,7 +325,7 @@ def test_binding_refuses_before_any_call():
         qift.KV4Pages(*(qift.KV4(torch.zeros(2, 8, 16, 64, dtype=torch.uint8), torch.zeros(2, 8, 16), torch.zeros(2, 8, 16))
                         for _ in range(2)))
     with pytest.raises(TypeError):
-        qift._rows(torch.zeros(3, 8, 128, dtype=torch.float16), torch.float16, 8, "k")
+        qift._rows(torch.zeros(3, 8, 128, dtype=torch.float16), 0, torch.float16, (3, 8, 128), "k")
 
 
 # ---- the oracle ---------------------------------------------------------------------------------------------------
