@@ -88,10 +88,12 @@ QIFT_HD uint64_t tree_bits(int32_t d0, uint64_t w0, uint64_t w1) {
 // How the attention cuts its work.  A workgroup takes a block of 16 rt query rows (a row is a node and a head of the KV
 // head's group) of one KV head and sequence at a time (a unit), over tokens in rounds of 256: 64 for each of its four
 // waves.  Few units: the rounds of all units, in order, are dealt out evenly to `shares` workgroups a block of rows, whatever the
-// sequences' lengths are; a unit that more than one share covers is joined from partial records.  Many units: one
-// workgroup takes a unit whole.
+// sequences' lengths are; a unit that more than one share covers is joined from partial records.  Beginning and ending a
+// unit takes a workgroup longer than a round, so a unit is dealt out as its rounds and kBegin more before them (32
+// ragged sequences of 8 heads, where a share may have eight short units: 52 us with 0, 46 with 1, 45 with 2).  Many units: one workgroup takes a unit whole.
 constexpr int kStep = 64, kWaves = 4, kRound = kStep * kWaves;
 constexpr int kMostShared = 512;   // sequences whose rounds are dealt out (every workgroup adds them up)
+constexpr int kBegin = 2;
 struct Plan {
   int32_t rt, blocks;   // row tiles of a workgroup, blocks of a KV head's rows
   int32_t shares;       // workgroups of a block of rows; 0: one to a unit
@@ -106,19 +108,25 @@ inline Plan plan(int64_t B, int32_t Hkv, int32_t G, int32_t max_nodes, int64_t m
   p.shares = 0;
   if (rounds > 1 && B <= kMostShared && units * p.blocks < 1024) {
     int64_t n = 512 / p.blocks;                 // two workgroups to each of 256 CUs
-    if (n > units * rounds) n = units * rounds;
+    if (n > units * (rounds + kBegin)) n = units * (rounds + kBegin);
     p.shares = n < 1 ? 1 : (int32_t)n;
   }
   return p;
 }
-// Share i of n covers the rounds [first_round(i), first_round(i + 1)) of W; round r lies in share_of(r).  No share is
-// empty: there are at most as many as rounds.
+// What is dealt out: the slots of all units, kBegin and its rounds for each.  Share i of n has the slots [first_slot(i),
+// first_slot(i + 1)) of W, at least one; of a unit whose slots it has from lo to hi - 1 (counted in the unit) it takes the
+// rounds round_at(lo) .. round_at(hi) - 1, if any.
+QIFT_HD int32_t slots_of(int32_t len) { return rounds_of(len) + kBegin; }
 QIFT_HD int32_t used_shares(int64_t W, int32_t shares) { return W < shares ? (int32_t)W : shares; }
-QIFT_HD int64_t first_round(int64_t W, int32_t n, int32_t i) { return W * i / n; }
-QIFT_HD int32_t share_of(int64_t W, int32_t n, int64_t r) { return (int32_t)(((r + 1) * n - 1) / W); }
+QIFT_HD int64_t first_slot(int64_t W, int32_t n, int32_t i) { return W * i / n; }
+QIFT_HD int32_t round_at(int32_t slot) { return slot > kBegin ? slot - kBegin : 0; }
 // Partial records: share i and unit u have number i + u (both grow along the rounds, so no two have the same), each
-// 128 sums per row, then (after all sums) the rows' references and sums of exponentials.
+// 128 sums per row, then (after all sums) the rows' references and sums of exponentials, then each unit's first and last
+// share.
 inline int64_t records(const Plan& p, int64_t B, int32_t Hkv) { return p.shares == 0 ? 0 : p.shares + B * Hkv; }
+inline int64_t workspace_words(const Plan& p, int64_t B, int32_t Hkv, int32_t G, int32_t max_nodes) {
+  return p.shares == 0 ? 0 : records(p, B, Hkv) * ((int64_t)max_nodes * G) * 130 + 2 * B * Hkv;
+}
 
 }  // namespace pages
 }  // namespace qift

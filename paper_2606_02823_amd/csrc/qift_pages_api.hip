@@ -82,7 +82,7 @@ size_t qift_kv4_attention_tree_workspace_bytes(int64_t B, int32_t Hq, int32_t Hk
                                                int64_t max_len) {
   if (!tree_shape_ok(B, Hq, Hkv, head_dim, max_nodes, max_len) || B == 0) return 0;
   const qift::pages::Plan p = qift::pages::plan(B, Hkv, Hq / Hkv, max_nodes, max_len);
-  return (size_t)qift::pages::records(p, B, Hkv) * ((size_t)max_nodes * (Hq / Hkv)) * 130 * sizeof(float);
+  return (size_t)qift::pages::workspace_words(p, B, Hkv, Hq / Hkv, max_nodes) * sizeof(float);
 }
 
 int qift_kv4_attention_tree(const qift_kv4_pages* cache, const void* q, int64_t q_stride, int32_t dtype, int64_t rows,

@@ -160,32 +160,46 @@ __device__ __forceinline__ uint16_t to_bits(float f, int bf16) {
 __device__ __forceinline__ pages::Seq sequence_of(ArgPtr a, int b) {
   return pages::sequence(a->starts[b], a->starts[b + 1], a->lens[b], a->rows, a->max_nodes, a->most);
 }
-// The rounds of all sequences before each one (times Hkv: before its first KV head), by the first wave; sequences without
-// nodes have none.
-__device__ __forceinline__ void add_rounds(ArgPtr a, int32_t* before, bool flag) {
+// All sequences, and the slots of those before each one (times Hkv: before its first KV head), by the first wave;
+// sequences without nodes have none.
+struct Sequences {
+  int32_t before[pages::kMostShared + 1];
+  int4 seq[pages::kMostShared];   // first row, nodes, length, context
+};
+// x of the lane and all lanes below it
+__device__ __forceinline__ int32_t running_sum(int32_t x) {
+#define QIFT_SUM(CTRL, ROWS) x += __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false)
+  QIFT_SUM(0x111, 0xf);   // row_shr 1, 2, 4, 8
+  QIFT_SUM(0x112, 0xf);
+  QIFT_SUM(0x114, 0xf);
+  QIFT_SUM(0x118, 0xf);
+  QIFT_SUM(0x142, 0xa);   // row_bcast 15 into rows 1 and 3, 31 into rows 2 and 3
+  QIFT_SUM(0x143, 0xc);
+#undef QIFT_SUM
+  return x;
+}
+__device__ __forceinline__ void add_slots(ArgPtr a, Sequences& all, bool flag) {
   if (threadIdx.x < 64) {
     int32_t sum = 0;
-    if (threadIdx.x == 0) before[0] = 0;
+    if (threadIdx.x == 0) all.before[0] = 0;
     const int B = a->B;
     for (int b0 = 0; b0 < B; b0 += 64) {
       const int b = b0 + (int)threadIdx.x;
       int32_t r = 0;
       if (b < B) {
         const pages::Seq sq = sequence_of(a, b);
-        r = sq.n > 0 ? pages::rounds_of(sq.len) : 0;
+        r = sq.n > 0 ? pages::slots_of(sq.len) : 0;
+        all.seq[b] = make_int4(sq.row0, sq.n, sq.len, sq.ctx);
         if (flag && sq.bad) dev::flag_error(a->err, kDevErrIndex);
       }
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const int32_t up = __shfl_up(r, d);
-        if ((int)threadIdx.x >= d) r += up;
-      }
-      if (b < B) before[b + 1] = sum + r;
-      sum += __shfl(r, 63);
+      r = running_sum(r);
+      if (b < B) all.before[b + 1] = sum + r;
+      sum += __builtin_amdgcn_readlane(r, 63);
     }
   }
   __syncthreads();
 }
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 // A run of rounds of one unit for the 16 RT rows from r0 on; whole: the run is all of the unit, so its result is final.
 struct Run {
@@ -211,6 +225,59 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
   const int32_t t_lo = run.lo * kRound;
   int32_t t_hi = run.hi * kRound;
 
+  const ArgPtr a = arguments();
+  {
+    const int32_t end = pages::last_token(sq, a->visible != nullptr, group_of(a), 16 * RT, r0 / (16 * RT));
+    if (end < t_hi) t_hi = end;
+  }
+  const int32_t* table = a->table + (int64_t)b * a->table_pages;
+  const uint8_t *kc = a->kc, *kz = a->kz, *vc = a->vc, *vz = a->vz;
+  const float *ks = a->ks, *vs = a->vs;
+  const pages::Div tiles = tiles_of(a);
+  const uint32_t pool_pages = a->pool_pages, Hkv = (uint32_t)a->Hkv;
+  auto entry = [&](int32_t t0) {   // the table's entry of token t0 + lane (anything for a token that is not there)
+    const int32_t t = t0 + lane;
+    return table[t < t_hi ? pages::table_index((uint32_t)t, tiles) : 0u];
+  };
+  bool bad = false;            // a table entry that names no page
+  auto rows_of = [&](int32_t t0, int32_t e) {
+    const int32_t t = t0 + lane;
+    Rows r;
+    r.ok = t < t_hi && (uint32_t)e < pool_pages;
+    bad |= t < t_hi && !r.ok;
+    r.row = r.ok ? pages::token_row((uint32_t)t, (uint32_t)e, Hkv, (uint32_t)kv, tiles) : 0u;
+    return r;
+  };
+  // A step's loads.  Its value codes, scales and zero-points go to LDS when it begins, its key codes are used from
+  // registers; the next step's are sent once they are, without a branch (a step past the end reads the cache's first
+  // rows).  A tile of 16 tokens is 1 KB from its first row on (a page holds whole tiles): a uniform address and a fixed
+  // offset of the lane.
+  uint4 vw[4], kw[4];
+  float ksl, vsl;
+  uint32_t kzl, vzl;
+  Rows cur{0, false};
+  int32_t ahead = 0;           // the next step's table entry
+  const uint32_t koff = 64u * (uint32_t)c + 16u * (uint32_t)kg, voff = 16u * (uint32_t)lane;
+  auto load = [&](const Rows& r) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint64_t first = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)r.row, 16 * j) * (kD / 2);
+      vw[j] = *reinterpret_cast<const uint4*>(vc + first + voff);
+      kw[j] = *reinterpret_cast<const uint4*>(kc + first + koff);
+    }
+    ksl = ks[r.row];
+    vsl = vs[r.row];
+    kzl = kz[r.row];
+    vzl = vz[r.row];
+  };
+
+  int32_t t0 = t_lo + wave * kStep;
+  if (t0 < t_hi) {
+    cur = rows_of(t0, entry(t0));
+    ahead = entry(t0 + kRound);
+    load(cur);
+  }
+
   // ---- the queries: B operands, element e of step st is dimension 32 kg + 8 st + kNib[e] of row c
   v8h qb[RT][4];
   float rowf[RT];      // bf16 rows brought into fp16's range by a power of two: the factor that takes it back
@@ -222,8 +289,6 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
   const int G = a->G, nrows = sq.n * G;
   const uint16_t* q = a->q;
   const int64_t stride = a->q_stride;
-  const int32_t end = pages::last_token(sq, a->visible != nullptr, group, 16 * RT, r0 / (16 * RT));
-  if (end < t_hi) t_hi = end;
   const bool bf16 = a->bf16 != 0;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
@@ -284,48 +349,6 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
   const Bits bits = code_bits();
   bool direct = false;         // the sum of exponentials is taken of the scores, not of the weights
   Stage& sg = lds.stage[wave];
-  const ArgPtr a = arguments();
-  const int32_t* table = a->table + (int64_t)b * a->table_pages;
-  const uint8_t *kc = a->kc, *kz = a->kz, *vc = a->vc, *vz = a->vz;
-  const float *ks = a->ks, *vs = a->vs;
-  const pages::Div tiles = tiles_of(a);
-  const uint32_t pool_pages = a->pool_pages, Hkv = (uint32_t)a->Hkv;
-  auto entry = [&](int32_t t0) {   // the table's entry of token t0 + lane (anything for a token that is not there)
-    const int32_t t = t0 + lane;
-    return table[t < t_hi ? pages::table_index((uint32_t)t, tiles) : 0u];
-  };
-  bool bad = false;            // a table entry that names no page
-  auto rows_of = [&](int32_t t0, int32_t e) {
-    const int32_t t = t0 + lane;
-    Rows r;
-    r.ok = t < t_hi && (uint32_t)e < pool_pages;
-    bad |= t < t_hi && !r.ok;
-    r.row = r.ok ? pages::token_row((uint32_t)t, (uint32_t)e, Hkv, (uint32_t)kv, tiles) : 0u;
-    return r;
-  };
-  // A step's loads.  Its value codes, scales and zero-points go to LDS when it begins, its key codes are used from
-  // registers; the next step's are sent once they are, without a branch (a step past the end reads the cache's first
-  // rows).  A tile of 16 tokens is 1 KB from its first row on (a page holds whole tiles): a uniform address and a fixed
-  // offset of the lane.
-  uint4 vw[4], kw[4];
-  float ksl, vsl;
-  uint32_t kzl, vzl;
-  Rows cur;
-  int32_t ahead;               // the next step's table entry
-  const uint32_t koff = 64u * (uint32_t)c + 16u * (uint32_t)kg, voff = 16u * (uint32_t)lane;
-  auto load = [&](const Rows& r) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint64_t first = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)r.row, 16 * j) * (kD / 2);
-      vw[j] = *reinterpret_cast<const uint4*>(vc + first + voff);
-      kw[j] = *reinterpret_cast<const uint4*>(kc + first + koff);
-    }
-    ksl = ks[r.row];
-    vsl = vs[r.row];
-    kzl = kz[r.row];
-    vzl = vz[r.row];
-  };
-
   auto step = [&](int32_t t0) {
     const uint64_t there = __ballot(cur.ok);
     // ---- stage the step's scales, zero-points and value codes (a wave's LDS operations keep their order)
@@ -526,13 +549,7 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
     __builtin_amdgcn_wave_barrier();
     cur = nxt;
   };
-  int32_t t0 = t_lo + wave * kStep;
-  if (t0 < t_hi) {
-    cur = rows_of(t0, entry(t0));
-    ahead = entry(t0 + kRound);
-    load(cur);
-    for (; t0 < t_hi; t0 += kRound) step(t0);
-  }
+  for (; t0 < t_hi; t0 += kRound) step(t0);
 
   const ArgPtr z = arguments();
   if (bad) dev::flag_error(z->err, kDevErrIndex);
@@ -604,7 +621,7 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
 template <int RT>
 __global__ __launch_bounds__(256, 2) void k_tree(TreeArgs) {
   __shared__ __attribute__((aligned(16))) Tree<RT> sh;
-  __shared__ int32_t before[pages::kMostShared + 1];
+  __shared__ Sequences all;
   const ArgPtr a = arguments();
   // blocks of rows over the same tokens are 8 workgroups apart: one XCD, whose L2 then holds the tokens
   const uint32_t per = 8u * (uint32_t)a->blocks;
@@ -626,84 +643,112 @@ __global__ __launch_bounds__(256, 2) void k_tree(TreeArgs) {
     return;
   }
   if (i >= (uint32_t)a->shares) return;
-  add_rounds(a, before, blockIdx.x == 0);
-  const int64_t W = (int64_t)__builtin_amdgcn_readfirstlane(before[a->B]) * a->Hkv;
+  add_slots(a, all, blockIdx.x == 0);
+  const int B = a->B, Hkv = a->Hkv;
+  const int64_t W = (int64_t)uniform(all.before[B]) * Hkv;
   const int32_t shares = pages::used_shares(W, a->shares);
   if ((int32_t)i >= shares) return;
-  int64_t pos = pages::first_round(W, shares, (int32_t)i);
-  const int64_t stop = pages::first_round(W, shares, (int32_t)i + 1);
-  // the sequence of the share's first round: the last one with no more rounds before it (one without rounds has as
-  // many before it as the next)
+  int64_t pos = pages::first_slot(W, shares, (int32_t)i);
+  const int64_t stop = pages::first_slot(W, shares, (int32_t)i + 1);
+  // the sequence of the share's first slot: as many as have all their slots before it (those without slots too)
   int b = 0;
-  for (int b0 = 0; b0 < a->B; b0 += 64) {
+  for (int b0 = 0; b0 < B; b0 += 64) {
     const int x = b0 + (int)(threadIdx.x & 63);
-    b += __popcll(__ballot(x < a->B && (int64_t)before[x + 1] * a->Hkv <= pos));
+    b += __popcll(__ballot(x < B && (int64_t)all.before[x + 1] * Hkv <= pos));
   }
-  b = __builtin_amdgcn_readfirstlane(b);
-  for (; pos < stop; ++b) {
-    const int32_t first = __builtin_amdgcn_readfirstlane(before[b]), n = __builtin_amdgcn_readfirstlane(before[b + 1]) - first;
-    if (n == 0) continue;
-    const pages::Seq sq = sequence_of(a, b);
+  for (b = uniform(b); pos < stop; ++b) {
+    const int4 q = all.seq[b];
+    const pages::Seq sq = {uniform(q.x), uniform(q.y), uniform(q.z), uniform(q.w), false};
+    if (sq.n == 0) continue;
+    const int32_t first = uniform(all.before[b]), rounds = pages::rounds_of(sq.len), n = pages::slots_of(sq.len);
     run.b = b;
-    for (run.kv = (int)((pos - (int64_t)first * a->Hkv) / n); run.kv < a->Hkv && pos < stop; ++run.kv) {
-      const int64_t at = (int64_t)first * a->Hkv + (int64_t)run.kv * n;
-      run.lo = (int32_t)(pos - at);
-      run.hi = stop - at < n ? (int32_t)(stop - at) : n;
-      run.whole = run.lo == 0 && run.hi == n;
-      run.record = (int64_t)i + (int64_t)b * a->Hkv + run.kv;
+    for (run.kv = (int)((uint32_t)(pos - (int64_t)first * Hkv) / (uint32_t)n); run.kv < Hkv && pos < stop; ++run.kv) {
+      const int64_t at = (int64_t)first * Hkv + (int64_t)run.kv * n;
+      const int32_t hi = stop - at < n ? (int32_t)(stop - at) : n;
+      run.lo = pages::round_at((int32_t)(pos - at));
+      run.hi = pages::round_at(hi);
+      pos = at + hi;
+      if (run.hi == run.lo) continue;
+      run.whole = run.lo == 0 && run.hi == rounds;
+      run.record = (int64_t)i + (int64_t)b * Hkv + run.kv;
+      if (block == 0 && threadIdx.x == 0) {   // which shares have the unit, for k_tree_merge
+        int32_t* units = reinterpret_cast<int32_t*>(a->part + a->records * (kD + 2)) + 2 * ((int64_t)b * Hkv + run.kv);
+        if (run.lo == 0) units[0] = (int32_t)i;
+        if (run.hi == rounds) units[1] = (int32_t)i;
+      }
       if (run.r0 < sq.n * a->G) {
         tree_run<RT>(sh, sq, run);
         __syncthreads();
       }
-      pos = at + run.hi;
     }
   }
 }
 
 // out = sum_i 2^(m_i - M) sums_i / sum_i 2^(m_i - M) l_i over the shares i that cover a row's unit, where there are more
-// than one.  32 lanes of four dimensions take a row, or `slices` times 32 lanes share its records.
+// than one.  32 lanes of four dimensions take a row, or `slices` times 32 lanes share its records, four at a time with
+// every load sent before the first is used (the call's second kernel mostly waits: each wait in a row costs it about
+// a microsecond of its four).
+constexpr int kJoin = 4;
 __global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a, int32_t slices) {
-  __shared__ int32_t before[pages::kMostShared + 1];
-  __shared__ v4f sum[8][32];
-  const ArgPtr p = arguments();
+  __shared__ v4f sums[8][32];
+  __shared__ float stats[2][8];
   const int lane = threadIdx.x & 31, slot = threadIdx.x >> 5;
   const int kv = blockIdx.y, b = blockIdx.z;
-  const pages::Seq sq = sequence_of(p, b);
+  const int64_t unit = (int64_t)b * a.Hkv + kv, R = (int64_t)a.max_nodes * a.G;
+  const int32_t* units = reinterpret_cast<const int32_t*>(a.part + a.records * (kD + 2)) + 2 * unit;
+  const int32_t i0 = units[0], count = units[1] - i0 + 1;   // (of a sequence without nodes: not written, and not used)
+  const pages::Seq sq = sequence_of(arguments(), b);
   const int nrows = sq.n * a.G, first = (int)blockIdx.x * (8 / slices);
-  if (first >= nrows) return;
-  add_rounds(p, before, false);
-  const int64_t W = (int64_t)__builtin_amdgcn_readfirstlane(before[a.B]) * a.Hkv;
-  const int32_t n = before[b + 1] - before[b];
-  const int64_t at = (int64_t)before[b] * a.Hkv + (int64_t)kv * n;
-  const int32_t shares = pages::used_shares(W, a.shares);
-  const int32_t i0 = pages::share_of(W, shares, at), count = pages::share_of(W, shares, at + n - 1) - i0 + 1;
-  if (count == 1) return;
+  if (first >= nrows || count == 1) return;
   const int r = first + slot / slices, slice = slot % slices;
   const bool in = r < nrows;
   v4f acc = {0.f, 0.f, 0.f, 0.f};
-  float L = 0.f;
+  float M = kLowest, L = 0.f;
   if (in) {
-    const int64_t R = (int64_t)a.max_nodes * a.G, rec = (i0 + (int64_t)b * a.Hkv + kv) * R + r;
+    const int64_t rec = (i0 + unit) * R + r;
     const float* st = a.part + a.records * kD + 2 * rec;
-    float M = kLowest;
-    for (int32_t i = lane; i < count; i += 32) M = fmaxf(M, st[2 * R * i]);
-#pragma unroll
-    for (int d = 16; d; d >>= 1) M = fmaxf(M, __shfl_xor(M, d));
-    for (int32_t i = lane; i < count; i += 32) L += scaled(st[2 * R * i + 1], st[2 * R * i] - M);
-#pragma unroll
-    for (int d = 16; d; d >>= 1) L += __shfl_xor(L, d);
     const float* y = a.part + rec * kD + 4 * lane;
-#pragma unroll 4
-    for (int32_t i = slice; i < count; i += slices) {
-      const float f = __builtin_amdgcn_exp2f(st[2 * R * i] - M);
-      acc += *reinterpret_cast<const v4f*>(y + R * kD * i) * f;
+    for (int32_t c0 = slice; c0 < count; c0 += slices * kJoin) {
+      v4f o[kJoin];
+      float m[kJoin], l[kJoin];
+#pragma unroll
+      for (int j = 0; j < kJoin; ++j) {
+        const int32_t c = c0 + slices * j < count ? c0 + slices * j : c0;   // past the last: the first again, without weight
+        o[j] = *reinterpret_cast<const v4f*>(y + R * kD * c);
+        m[j] = st[2 * R * c];
+        l[j] = st[2 * R * c + 1];
+      }
+      float top = M;
+#pragma unroll
+      for (int j = 0; j < kJoin; ++j) top = fmaxf(top, m[j]);
+      acc *= __builtin_amdgcn_exp2f(M - top);
+      L = scaled(L, M - top);
+#pragma unroll
+      for (int j = 0; j < kJoin; ++j)
+        if (c0 + slices * j < count) {
+          acc += o[j] * __builtin_amdgcn_exp2f(m[j] - top);
+          L += scaled(l[j], m[j] - top);
+        }
+      M = top;
     }
   }
   if (slices > 1) {
-    sum[slot][lane] = acc;
+    sums[slot][lane] = acc;
+    if (lane == 0) {
+      stats[0][slot] = M;
+      stats[1][slot] = L;
+    }
     __syncthreads();
     if (slice) return;
-    for (int s = 1; s < slices; ++s) acc += sum[slot + s][lane];
+    float top = M;
+    for (int s = 1; s < slices; ++s) top = fmaxf(top, stats[0][slot + s]);
+    acc *= __builtin_amdgcn_exp2f(M - top);
+    L = scaled(L, M - top);
+    for (int s = 1; s < slices; ++s) {
+      const float m = stats[0][slot + s];
+      acc += sums[slot + s][lane] * __builtin_amdgcn_exp2f(m - top);
+      L += scaled(stats[1][slot + s], m - top);
+    }
   }
   if (!in) return;
   const int nd = (int)pages::quotient((uint32_t)r, a.group);
@@ -759,9 +804,9 @@ hipError_t launch_kv4_tree(const TreeCall& t, hipStream_t s) {
   hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.shares == 0) return e;
-  // the records of a row: about as many as shares to a unit, and one more; many are shared by 8 slices
+  // a row's records: about as many as there are shares to a unit, and one more
   const int64_t each = p.shares / (t.B * c.Hkv) + 2;
-  const int32_t slices = each > 16 ? 8 : each > 4 ? 4 : 2;
+  const int32_t slices = each <= kJoin ? 1 : each <= 2 * kJoin ? 2 : each <= 4 * kJoin ? 4 : 8;
   const int64_t R = (int64_t)t.max_nodes * G;
   const dim3 mgrid((unsigned)((R * slices + 7) / 8), (unsigned)c.Hkv, (unsigned)t.B);
   hipLaunchKernelGGL(k_tree_merge, mgrid, dim3(256), 0, s, a, slices);

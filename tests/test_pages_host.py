@@ -69,9 +69,17 @@ int main() {
       std::scanf("%lld %d", &W, &n);
       std::printf("%d\n", used_shares(W, n));
     } else if (!std::strcmp(what, "share")) {
-      long long W, r; int n, i;
-      std::scanf("%lld %d %d %lld", &W, &n, &i, &r);
-      std::printf("%lld %lld %d\n", (long long)first_round(W, n, i), (long long)first_round(W, n, i + 1), share_of(W, n, r));
+      long long W; int n, i;
+      std::scanf("%lld %d %d", &W, &n, &i);
+      std::printf("%lld %lld\n", (long long)first_slot(W, n, i), (long long)first_slot(W, n, i + 1));
+    } else if (!std::strcmp(what, "slots")) {
+      int len;
+      std::scanf("%d", &len);
+      std::printf("%d %d\n", rounds_of(len), slots_of(len));
+    } else if (!std::strcmp(what, "round")) {
+      int slot;
+      std::scanf("%d", &slot);
+      std::printf("%d\n", round_at(slot));
     }
   }
 }
@@ -190,40 +198,47 @@ def test_plan_covers_every_row(ask):
                       int(rng.integers(1, 257)), int(np.exp(rng.uniform(0, 19.4)))))
     for (_, B, Hkv, G, nodes, length), (rt, blocks, shares, records) in zip(lines, ask(lines)):
         assert rt in (1, 2, 4) and blocks * 16 * rt >= nodes * G > (blocks - 1) * 16 * rt
-        assert 0 <= shares <= B * Hkv * -(-length // 256) and (B <= 512 or shares == 0)
+        assert 0 <= shares <= B * Hkv * (-(-length // 256) + 2) and (B <= 512 or shares == 0)
         assert records == (shares + B * Hkv if shares else 0)
 
 
 def test_shares_cover_every_round_once(ask):
-    """The runs of units that the shares take, as the kernel walks them: every round once, the records' numbers
-    different and inside the workspace, and the shares that a unit is joined from those that took part of it."""
+    """The runs of units that the shares take, as the kernel walks them: every round once and in order, the records'
+    numbers different and inside the workspace, and the shares of a unit that have rounds of it next to each other (the
+    partial records of a unit are joined from its first share to its last)."""
     rng = np.random.default_rng(11)
-    for _ in range(60):
+    for _ in range(80):
         B, Hkv = int(rng.integers(1, 9)), int(rng.integers(1, 9))
-        rounds = rng.integers(0, 40, B) * rng.integers(0, 2, B)
-        W = int(rounds.sum()) * Hkv
-        n = int(rng.integers(1, 120))
+        lens = rng.integers(0, 256 * 30, B) * rng.integers(0, 2, B) // rng.choice([1, 1, 8])
+        nodes = rng.integers(0, 2, B)                                     # sequences without nodes have no slots
+        slots = np.array([g[1] for g in ask([("slots", int(t)) for t in lens])]) * nodes
+        rounds = np.array([g[0] for g in ask([("slots", int(t)) for t in lens])]) * nodes
+        assert (rounds[nodes > 0] == np.maximum(1, -(-lens[nodes > 0] // 256))).all()
+        W = int(slots.sum()) * Hkv
+        asked = int(rng.integers(1, 120))
         if W == 0:
             continue
-        asked, n = n, ask([("used", W, n)])[0][0]
+        n = ask([("used", W, asked)])[0][0]
         assert n == min(W, asked)
-        units = [(b * Hkv + kv, int(rounds[:b].sum()) * Hkv + kv * int(rounds[b]), int(rounds[b])) for b in range(B) for kv in range(Hkv)]
-        bounds = [g[:2] for g in ask([("share", W, n, i, 0) for i in range(n)])]
-        assert bounds[0][0] == 0 and all(lo < hi for lo, hi in bounds) and bounds[-1][1] == W and all(a[1] == b[0] for a, b in zip(bounds, bounds[1:]))
-        holds = [g[2] for g in ask([("share", W, n, 0, r) for r in range(W)])]
-        assert all(bounds[holds[r]][0] <= r < bounds[holds[r]][1] for r in range(W))
-        seen, numbers = np.zeros(W, int), set()
-        for u, at, k in units:
-            took = []
-            for i, (lo, hi) in enumerate(bounds):
-                lo, hi = max(lo, at), min(hi, at + k)
-                if lo < hi:
-                    seen[lo:hi] += 1
+        bounds = ask([("share", W, n, i) for i in range(n)])
+        assert bounds[0][0] == 0 and all(lo < hi for lo, hi in bounds) and bounds[-1][1] == W
+        assert all(a[1] == b[0] for a, b in zip(bounds, bounds[1:]))
+        at_slot = [g[0] for g in ask([("round", i) for i in range(int(slots.max()) + 1)])]
+        numbers = set()
+        for b in range(B):
+            for kv in range(Hkv):
+                at, k, u = int(slots[:b].sum()) * Hkv + kv * int(slots[b]), int(slots[b]), b * Hkv + kv
+                took, next_round = [], 0
+                for i, (lo, hi) in enumerate(bounds):
+                    lo, hi = max(lo, at), min(hi, at + k)
+                    if lo >= hi or at_slot[hi - at] == at_slot[lo - at]:
+                        continue
+                    assert at_slot[lo - at] == next_round
+                    next_round = at_slot[hi - at]
                     took.append(i)
                     assert 0 <= i + u < n + B * Hkv and i + u not in numbers
                     numbers.add(i + u)
-            assert took == ([] if k == 0 else list(range(holds[at], holds[at + k - 1] + 1))) or k == 0
-        assert (seen == 1).all()
+                assert next_round == rounds[b] and took == list(range(took[0], took[-1] + 1) if took else [])
 
 
 # ---- the C ABI ---------------------------------------------------------------------------------------------------
@@ -310,7 +325,7 @@ def test_tree_refusals(L):
                dict(work=MIS), dict(cache=pool(v_codes=MIS))):
         assert f(**kw) == E_ALIGN, kw
     need = ws(2, 32, 8, 128, 8, 3000)
-    assert need > 0 and need % (130 * 4) == 0
+    assert need > 2 * 8 * 8 and (need - 2 * 8 * 8) % (8 * 4 * 130 * 4) == 0   # records of rows, then a pair per unit
     assert f(work=None) == E_WS and f(size=need - 1) == E_WS and f(size=0) == E_WS
     assert f(B=0, q=None, table=None, starts=None, lens=None, out=None, work=None) == OK
     assert f(rows=0, q=None, out=None) == OK
