@@ -66,7 +66,7 @@ typedef struct {
  *   k_values, v_values   out, nullable (both or none): the values s (q - z) that the cache now
  *              stands for, [n][Hkv][128] in dtype (one rounding from fp32), for the attention of the
  *              prompt that is being written; zeros for a token that is not written.
- *   n = 0 does nothing.  Limits: n < 2^31, n * Hkv < 2^34.
+ *   n = 0 does nothing.  Limits: ceil(n / 16) * Hkv < 2^23.
  */
 int qift_kv4_append(const qift_kv4_pages *cache, const void *k, const void *v, int64_t k_stride,
                     int64_t v_stride, int32_t dtype, const int32_t *slots, int64_t n, void *k_values,
@@ -76,7 +76,7 @@ int qift_kv4_append(const qift_kv4_pages *cache, const void *k, const void *v, i
  * Read tokens back: k_values, v_values [n][Hkv][128] = s (code - z) of the given slots, computed in
  * fp32 and rounded once to dtype (QIFT_F16, QIFT_BF16, or QIFT_F32: the fp32 value itself).  A negative
  * slot gives zeros; a slot at or past pages * page zeros and QIFT_DEVERR_INDEX.  A slot may appear
- * any number of times.  n = 0 does nothing.  Limits: n < 2^31.
+ * any number of times.  n = 0 does nothing.  Limits: n <= 2^30 - 64.
  */
 int qift_kv4_read(const qift_kv4_pages *cache, const int32_t *slots, int64_t n, int32_t dtype,
                   void *k_values, void *v_values, qift_stream_t stream);
@@ -117,12 +117,16 @@ size_t qift_kv4_attention_tree_workspace_bytes(int64_t B, int32_t Hq, int32_t Hk
  *   workspace  device scratch of qift_kv4_attention_tree_workspace_bytes bytes (16-byte aligned;
  *              NULL where that is 0): partial sums of parts of long sequences.  It belongs to one call
  *              at a time: calls that overlap, two captured graphs among them, need their own.
- * Scores: products of exact fp16 operands (code - z, and the queries; bf16 queries are scaled by a
- * power of two per row, which keeps them exact down to 2^-28 of the row's largest) summed in fp32;
- * softmax statistics and sums in fp32; weights p s split into two fp16 parts (2^-21 relative).  Per
- * query head the result is within half a step of its type plus 1e-4 of the head's largest output.
+ * Scores: products of exact fp16 operands (code - z, and the queries; a bf16 row whose largest is outside
+ * [2^-4, 2^15) is scaled by a power of two, and of any bf16 row what is below 2^-17, or 2^-31 of a scaled
+ * row's largest, is off by 2^-25, or 2^-39, at most) summed in fp32; softmax statistics and sums in fp32;
+ * weights p s split into two fp16 parts (2^-21 relative).  The result is within half a step of its type and
+ * (2 (S + L + 1) + 1 + lens[b] / 256) 2^-21 of the KV head's largest value, S the largest |q| |k_hat| / sqrt(128)
+ * of the row and L the largest |log2| of a value scale that it sees: 2e-5 at S = 16, L = 3 and 256 tokens.
+ * Value scales under 2^-90 count as 2^-90.
  * B = 0 or rows = 0 does nothing.  Limits: 1 <= max_nodes <= 256, Hq a multiple of Hkv and
- * Hq / Hkv <= 64, B <= 65535, max_len < 2^28, rows < 2^31.  Up to two launches.
+ * Hq / Hkv <= 64, B <= 65535, max_len < 2^28, rows < 2^31, B * Hkv * ceil(max_nodes * Hq / Hkv / 16) < 2^23.
+ * Up to two launches.
  */
 int qift_kv4_attention_tree(const qift_kv4_pages *cache, const void *q, int64_t q_stride, int32_t dtype,
                             int64_t rows, const int32_t *table, int32_t table_pages, const int32_t *starts,

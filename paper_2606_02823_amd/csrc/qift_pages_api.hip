@@ -10,6 +10,7 @@ static_assert(QIFT_DEVERR_INDEX == qift::kDevErrIndex, "error bit");
 namespace {
 
 constexpr int64_t k31 = int64_t(1) << 31;
+constexpr int64_t kGroups = int64_t(1) << 24;   // workgroups along x: 256 threads each, fewer than 2^32 threads
 
 inline bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
@@ -36,7 +37,7 @@ bool tree_shape_ok(int64_t B, int32_t Hq, int32_t Hkv, int32_t head_dim, int32_t
   if (head_dim != 128 || B < 0 || B > 65535 || Hkv < 1 || Hkv > 65535 || Hq < Hkv || Hq % Hkv || Hq / Hkv > 64) return false;
   if (max_nodes < 1 || max_nodes > 256 || max_len < 1 || max_len >= (int64_t(1) << 28)) return false;
   const qift::pages::Plan p = qift::pages::plan(B < 1 ? 1 : B, Hkv, Hq / Hkv, max_nodes, max_len);
-  return ((p.shares ? p.shares : B * Hkv) + 8) * p.blocks < k31;
+  return ((p.shares ? p.shares : B * Hkv) + 8) * p.blocks < kGroups;
 }
 
 }  // namespace
@@ -51,7 +52,7 @@ int qift_kv4_append(const qift_kv4_pages* cache, const void* k, const void* v, i
   if (dtype != QIFT_F16 && dtype != QIFT_BF16) return QIFT_ERR_FORMAT;
   const int64_t width = (int64_t)cache->Hkv * 128;
   if (n < 0 || n >= k31 || k_stride < width || v_stride < width || k_stride >= k31 || v_stride >= k31) return QIFT_ERR_SHAPE;
-  if ((n + 15) / 16 * 2 * cache->Hkv >= k31) return QIFT_ERR_SHAPE;   // one workgroup to 16 tokens, a head and a side
+  if ((n + 15) / 16 * 2 * cache->Hkv >= kGroups) return QIFT_ERR_SHAPE;   // one to 16 tokens, a head and a side
   if (n == 0) return QIFT_OK;
   if (!k || !v || !slots || (!k_values) != (!v_values)) return QIFT_ERR_NULL;
   st = check_pointers(cache);
@@ -69,7 +70,7 @@ int qift_kv4_read(const qift_kv4_pages* cache, const int32_t* slots, int64_t n, 
   int st = check_shape(cache);
   if (st != QIFT_OK) return st;
   if (dtype != QIFT_F16 && dtype != QIFT_BF16 && dtype != QIFT_F32) return QIFT_ERR_FORMAT;
-  if (n < 0 || n >= k31) return QIFT_ERR_SHAPE;
+  if (n < 0 || (n + 63) / 64 >= kGroups) return QIFT_ERR_SHAPE;   // 64 tokens to a workgroup
   if (n == 0) return QIFT_OK;
   if (!slots || !k_values || !v_values) return QIFT_ERR_NULL;
   st = check_pointers(cache);

@@ -281,6 +281,8 @@ def test_append_refusals(L):
     for kw in (dict(n=-1), dict(n=2 ** 31), dict(ks=1023), dict(vs=0), dict(ks=-1024), dict(vs=2 ** 31),
                dict(cache=pool(pages=1, page=16, Hkv=65535), n=2 ** 20, ks=65535 * 128, vs=65535 * 128)):
         assert f(**kw) == E_SHAPE, kw
+    # workgroups of 256 threads along one axis of a launch: fewer than 2^32 threads
+    assert f(n=2 ** 24, k=None) == E_SHAPE and f(n=2 ** 24 - 16, k=None) == E_NULL
     for kw in (dict(k=None), dict(v=None), dict(slots=None), dict(kv=A), dict(vv=A), dict(cache=pool(v_zeros=None))):
         assert f(**kw) == E_NULL, kw
     for kw in (dict(k=MIS), dict(v=MIS), dict(ks=1028), dict(vs=1030), dict(slots=A + 2), dict(kv=MIS, vv=A),
@@ -297,6 +299,7 @@ def test_read_refusals(L):
         assert f(cache=pool(**bad)) == E_SHAPE, bad
     assert f(dt=3) == E_FORMAT
     assert f(n=-1) == E_SHAPE and f(n=2 ** 31) == E_SHAPE
+    assert f(n=2 ** 30, slots=None) == E_SHAPE and f(n=2 ** 30 - 64, slots=None) == E_NULL
     for kw in (dict(slots=None), dict(kv=None), dict(vv=None), dict(cache=pool(k_scales=None))):
         assert f(**kw) == E_NULL, kw
     for kw in (dict(slots=A + 1), dict(kv=MIS), dict(vv=MIS), dict(cache=pool(k_zeros=MIS))):
@@ -319,6 +322,9 @@ def test_tree_refusals(L):
                dict(nodes=257), dict(length=0), dict(length=2 ** 28), dict(rows=-1), dict(rows=2 ** 31), dict(tp=0), dict(qs=4095),
                dict(qs=2 ** 31)):
         assert f(**kw) == E_SHAPE, kw
+    # (512 workgroups to a sequence and KV head)
+    big = dict(cache=pool(Hkv=1), Hq=64, qs=64 * 128, nodes=256, length=256)
+    assert f(B=2 ** 15, q=None, **big) == E_SHAPE and f(B=2 ** 15 - 16, q=None, **big) == E_NULL
     for kw in (dict(q=None), dict(table=None), dict(starts=None), dict(lens=None), dict(out=None), dict(cache=pool(k_codes=None))):
         assert f(**kw) == E_NULL, kw
     for kw in (dict(q=MIS), dict(qs=4100), dict(out=MIS), dict(table=A + 2), dict(starts=A + 1), dict(lens=A + 2), dict(vis=A + 4),
