@@ -34,14 +34,14 @@ typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef int v2i __attribute__((ext_vector_type(2)));
 
-constexpr float kLowest = -1e30f;   // the reference of a row that has seen nothing: finite, below any score
+constexpr float kLowest = -0x1p127f;   // the reference of a row that has seen nothing: finite, below the scores of any queries
 constexpr float kSlack = 8.f;       // how far, as a power of two, a weight may pass 1 before the reference moves
 constexpr float kTop = 7.f;         // w at the reference is 2^kTop, so w < 2^(kSlack + kTop) = 2^15
 // A vector of zeros has scale 1 whatever the scales around it, so kLeast stands for it in the reference (and for smaller
-// scales: results below 2^-86 may be off).  Its p cannot be had from w, nor those of scales so far from 1 that w leaves
-// fp32's range under another token's reference: from the first such token on a wave takes the exponentials of the
-// scores too.
-constexpr float kLeast = 0x1p-90f, kFar = 0x1p60f;
+// scales: results below 2^-86 may be off).  Its w may then leave fp32's range where its p counts, and so may those of
+// scales far from 1 under another token's reference (within [2^-50, 2^50] a p that is lost so is 2^-33 of another at most):
+// from the first such token on a wave takes the p of a w that is 0 from the score.
+constexpr float kLeast = 0x1p-90f, kFar = 0x1p50f;
 
 // x 2^d, also where 2^d alone is no normal number
 __device__ __forceinline__ float scaled(float x, float d) {
@@ -347,13 +347,13 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
     for (int dt = 0; dt < 8; ++dt) o[rt][dt] = v4f{0.f, 0.f, 0.f, 0.f};
   }
   const Bits bits = code_bits();
-  bool direct = false;         // the sum of exponentials is taken of the scores, not of the weights
+  bool direct = false;         // a weight that is 0 need not mean that p is
   Stage& sg = lds.stage[wave];
   auto step = [&](int32_t t0) {
     const uint64_t there = __ballot(cur.ok);
     // ---- stage the step's scales, zero-points and value codes (a wave's LDS operations keep their order)
     {
-      float v = fmaxf(vsl, kLeast);
+      float v = vsl < kLeast ? kLeast : vsl;   // (NaN stays: w is NaN where it is seen)
       const bool unit = vsl == 1.f && vzl == 0, far = vsl < INFINITY && !(vsl > 1.f / kFar && vsl < kFar);
       if (__any(cur.ok && (unit || far))) {
         // (a lane's token is t0 + lane; load u holds 16 bytes of token 16 u + lane / 4)
@@ -369,7 +369,7 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
       }
       sg.ks[lane] = ksl * (0.088388347648318447f * 1.4426950408889634f);   // 1 / sqrt(128), log2 e
       sg.ls[lane] = __builtin_amdgcn_logf(v);
-      sg.rs[lane] = cur.ok && !direct && vsl < INFINITY ? __builtin_amdgcn_rcpf(v) : 0.f;   // (NaN: w is NaN where it is seen)
+      sg.rs[lane] = vsl < INFINITY ? __builtin_amdgcn_rcpf(v) : 0.f; 
       const _Float16 kzb = (_Float16)(1024.f + (float)kzl);
       sg.kz[lane] = __builtin_bit_cast(uint32_t, v2h{kzb, kzb});
       // token 16 j + 4 g + i goes to pair i of half j / 2 of lane group g, element j mod 2
@@ -481,7 +481,8 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            l[rt] += y[rt][j][i] > -INFINITY ? __builtin_amdgcn_exp2f(y[rt][j][i] - l4[i] - m[rt]) : 0.f;
+            l[rt] += y[rt][j][i] > -INFINITY && __builtin_amdgcn_exp2f(y[rt][j][i] - m[rt]) == 0.f
+                         ? __builtin_amdgcn_exp2f(y[rt][j][i] - l4[i] - m[rt]) : 0.f;
       }
     }
 #pragma unroll

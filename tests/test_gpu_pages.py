@@ -326,6 +326,61 @@ def test_values_whose_scale_grows_along_the_sequence(Q):
     c.check(c.run(Q), "growing")
 
 
+def test_value_scales_of_every_size_in_one_sequence(Q):
+    """Neighbouring tokens' value scales up to 2^166 apart: the large ones decide the sums, all count for the weights."""
+    rng = np.random.default_rng(5)
+    vs = 10.0 ** rng.choice([-25, -12, 0, 12, 25], size=(1700, 4, 1))
+    for nodes in (1, 9):
+        c = Case(Q, 93 + nodes, [(nodes, 1700)], 16, 4, 64, torch.bfloat16, vscale=vs)
+        c.check(c.run(Q), f"mixed, {nodes} nodes")
+        # far scales in the last tokens only: what a wave summed before them stands
+        c = Case(Q, 95 + nodes, [(nodes, 1700)], 16, 4, 64, torch.bfloat16, vscale=np.where(np.arange(1700) < 1650, 1.0, 1e-22)[:, None, None])
+        c.check(c.run(Q), f"far ones last, {nodes} nodes")
+
+
+def test_many_sequences_of_any_length(Q):
+    """Shares that hold several sequences, ends and beginnings of others, and none of a sequence without nodes; and more
+    sequences than are dealt out, a workgroup to each."""
+    rng = np.random.default_rng(6)
+    lens = [int(t) for t in np.r_[rng.integers(1, 300, 40), 2300, 1, 0, rng.integers(200, 1100, 20), 4000]]
+    seqs = [(0 if b % 7 == 3 else min(t, 1 + b % 3), t) for b, t in enumerate(lens)]
+    c = Case(Q, 97, seqs, 32, 8, 32, torch.float16)
+    c.check(c.run(Q), "ragged")
+    seqs = [(min(t, 1 + b % 2), t) for b, t in enumerate(int(t) for t in rng.integers(0, 330, 530))]
+    c = Case(Q, 98, seqs, 4, 1, 16, torch.bfloat16)
+    c.check(c.run(Q), "a workgroup each")
+    c = Case(Q, 99, seqs[:510], 4, 1, 16, torch.bfloat16)
+    c.check(c.run(Q), "dealt out")
+    assert Q.device_error() == 0
+
+
+def test_scores_far_from_zero(Q):
+    """One seen token is the whole softmax whatever its score: here past -1e31, and past 1e31."""
+    only = np.array([[False, True], [False, True]])
+    c = Case(Q, 100, [(2, 2)] * 6, 8, 2, 16, torch.bfloat16, [only] * 6)
+    rows = lambda x: torch.from_numpy(np.stack([t[1] for t in x for _ in range(2)])).repeat_interleave(4, dim=1)  # noqa: E731
+    ref = rows(c.v)
+    assert ref.any(dim=-1).all()
+    for sign in (-1.0, 1.0):
+        c.q = (sign * 1e32 * rows(c.k)).to(torch.bfloat16)          # a score of sign |k|^2 1e32 / sqrt(128)
+        y = c.run(Q).float().cpu()
+        assert (y - ref).abs().le(ref.abs() * (2.0 ** -8 + 2.0 ** -20)).all(), sign
+
+
+def test_a_scale_that_is_nan_shows_where_it_is_seen(Q):
+    """Node 4 of a chain has a NaN value scale in one KV head: rows 4 and on are NaN in that head's group, no other."""
+    for t in (60, 1500):
+        c = Case(Q, 101, [(9, t)], 16, 4, 64, torch.float16)
+        want = c.run(Q)
+        slot = int(c.slots(0, np.array([t - 5]))[0])
+        c.cache.v.scales[slot // 64, 2, slot % 64] = float("nan")
+        got = c.run(Q)
+        assert torch.isnan(got[4:, 8:12]).all()
+        keep = torch.ones((9, 16), dtype=torch.bool, device="cuda")
+        keep[4:, 8:12] = False
+        assert torch.equal(got[keep], want[keep])
+
+
 def test_rows_that_see_nothing_and_rows_behind_the_last(Q):
     rng = np.random.default_rng(3)
     masks = [random_tree(rng, 6), random_tree(rng, 4), np.zeros((3, 3), dtype=bool)]
