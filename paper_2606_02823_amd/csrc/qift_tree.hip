@@ -9,11 +9,11 @@
 // sequence are joined by k_tree_merge.
 //
 // Per step, with c = lane mod 16 and kg = lane / 16:
-//   scores   D[token][row] on the f16 MFMA, A = 16 tokens x 32 dimensions of code - z (exact), B = the queries; lane
-//            (c, kg) receives tokens 16 j + 4 kg + i (j, i = 0 .. 3) of row c;
+//   scores   D[token][row] on the f16 MFMA, A = 16 tokens x 32 dimensions of codes (exact), B = the queries, on top of -z
+//            times the row's sum of queries; lane (c, kg) receives tokens 16 j + 4 kg + i (j, i = 0 .. 3) of row c;
 //   softmax  in the lane.  What meets the value codes is w_t = p_t s_t, so the reference m of a row is a bound of
 //            score + log2 s, not of the score: w = 2^(score + log2 s - m) then fits fp16 whatever the scales are, p = w / s
-//            goes into the sum of exponentials, and sum w (code - z) / sum p is the result.  The reference only moves when
+//            goes into the sum of exponentials, and (sum w code - sum w z) / sum p is the result.  The reference only moves when
 //            it is passed by 2^8, so most steps need no reduction across lanes and no rescaling;
 //   values   D[dimension][row] += A[dimension][token] B[token][row], B = w as two fp16 parts (2^-21 relative), which the
 //            lane holds in place: the contraction's order of tokens is the one the scores left, and the transposing
@@ -91,27 +91,29 @@ __device__ __forceinline__ int thread_again() {
   return t;
 }
 
-// Eight codes of a word less their zero-points, as exact fp16: a code in bits 0-3 of a half under the exponent of
-// 1024, one in bits 4-7 under that of 64; then the base, 1024 or 64 plus the zero-point, is subtracted.  Element e is
-// nibble kNib[e].
+// Eight codes of a word as fp16 operands.  A code in the lowest bits of a half is the subnormal number code 2^-24, which the
+// matrix instructions take exactly, so no exponent is put on and no base taken off; where a code stands four bits up it is
+// 16 times that (the key side has the queries there 16 times smaller; the value side shifts, as weights would lose bits).
+// Zero-points are left out and their share is taken from the sums by one more product: the loop is bound by the instructions
+// it issues, and unpacking was the largest part of them (with an exponent and a subtraction to each pair of codes: 16 trees
+// of 64 nodes 259 us, now 246; 32 ragged sequences of one token 45, now 43).  Element e is nibble kNib[e].
 constexpr int kNib[8] = {0, 4, 1, 5, 2, 6, 3, 7};
-// Masks and exponents as register values the compiler knows nothing of: with literals it takes an and and an or for each
-// pair of codes, from registers the one instruction that does both.
-struct Bits {
-  uint32_t m0, m1, e10, e6;
-};
-__device__ __forceinline__ Bits code_bits() {
-  Bits k = {0x000F000Fu, 0x00F000F0u, 0x64006400u, 0x54005400u};
-  asm("" : "+s"(k.m0), "+s"(k.m1), "+v"(k.e10), "+v"(k.e6));
-  return k;
-}
-__device__ __forceinline__ v8h unpack(uint32_t w, const Bits& k, v2h b0, v2h b1, v2h b2, v2h b3) {
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ v8h key_codes(uint32_t w) {   // elements 2, 3, 6 and 7 (kUp) times 16
   const uint32_t w8 = w >> 8;
-  const v2h h0 = __builtin_bit_cast(v2h, (w & k.m0) | k.e10) - b0;
-  const v2h h1 = __builtin_bit_cast(v2h, (w & k.m1) | k.e6) - b1;
-  const v2h h2 = __builtin_bit_cast(v2h, (w8 & k.m0) | k.e10) - b2;
-  const v2h h3 = __builtin_bit_cast(v2h, (w8 & k.m1) | k.e6) - b3;
-  return v8h{h0[0], h0[1], h1[0], h1[1], h2[0], h2[1], h3[0], h3[1]};
+  return __builtin_bit_cast(v8h, v4u{w & 0x000F000Fu, w & 0x00F000F0u, w8 & 0x000F000Fu, w8 & 0x00F000F0u});
+}
+__device__ __forceinline__ constexpr bool kUp(int e) { return (e & 2) != 0; }
+__device__ __forceinline__ v8h value_codes(uint32_t w) {
+  return __builtin_bit_cast(v8h, v4u{w & 0x000F000Fu, (w >> 4) & 0x000F000Fu, (w >> 8) & 0x000F000Fu, (w >> 12) & 0x000F000Fu});
+}
+
+// One of the two elements of a word of queries
+template <bool BF16>
+__device__ __forceinline__ float element(uint32_t w, bool high) {
+  if constexpr (BF16) return __uint_as_float(high ? w & 0xFFFF0000u : w << 16);
+  const v2h h = __builtin_bit_cast(v2h, w);
+  return (float)(high ? h[1] : h[0]);
 }
 
 // Largest of three, in one instruction (fmaxf would first quiet each operand); a NaN is passed over
@@ -142,8 +144,8 @@ struct Rows {
 struct Stage {
   uint32_t v[kStep * kD / 8];   // value codes, 64 bytes a token, 16-byte pieces of row r at piece ^ (r / 16)
   float ks[kStep], ls[kStep], rs[kStep];   // key scale log2 e / sqrt(128); log2 and reciprocal of the value scale
-  uint32_t kz[kStep];           // 1024 + key zero-point as fp16, twice
-  _Float16 vz[kStep];           // 1024 (tokens of odd place in their four: 64) + value zero-point, in the order of use
+  v4u kz[kStep];                // twice the key zero-point, eight times: fp16 of 2^-23 its size
+  _Float16 vz[kStep];           // value zero-point, fp16 of 2^-24 its size, in the order of use
 };
 constexpr int kPad = kD + 4;
 union Lds {
@@ -151,7 +153,7 @@ union Lds {
   float sum[kWaves][16][kPad];
 };
 
-__device__ __forceinline__ uint16_t to_bits(float f, int bf16) {
+__device__ __forceinline__ uint16_t to_bits(float f, bool bf16) {
   if (!bf16) return __builtin_bit_cast(uint16_t, (_Float16)f);
   const uint32_t u = __float_as_uint(f);
   return (uint16_t)(f == f ? (u + 0x7FFFu + ((u >> 16) & 1u)) >> 16 : (u >> 16) | 0x40u);
@@ -213,9 +215,10 @@ template <int RT>
 struct Tree {
   Lds lds;
   float stat[2][kWaves][16 * RT];   // reference, sum of exponentials
+  float back[16 * RT];
 };
 
-template <int RT>
+template <int RT, bool BF16>
 __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, const Run& run) {
   const int lane = thread_again() & 63, c = lane & 15, kg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -278,10 +281,13 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
     load(cur);
   }
 
-  // ---- the queries: B operands, element e of step st is dimension 32 kg + 8 st + kNib[e] of row c
+  // ---- the queries: B operands, element e of step st is dimension 32 kg + 8 st + kNib[e] of row c, 16 times where the code
+  // is not.  fp16 holds them where the row's largest is in [2^-4, 2^5), or brought to [2^4, 2^5) by a power of two: what is
+  // below 2^-14 (bf16: 2^-17) then is off by 2^-25 at most.  What zero-points contribute, -z sum q, comes from a product of
+  // its own: -8 sum q, at most 2^15, as three fp16 parts (2^-25 off at most) in elements 0 .. 2 of lane group 0.
   v8h qb[RT][4];
-  float rowf[RT];      // bf16 rows brought into fp16's range by a power of two: the factor that takes it back
-  bool ranged = false; // whether any row is one
+  v8h qz[RT];
+  bool ranged = false; // whether any row has a power of two to be taken back (sh.back; all waves write the same)
   int32_t node[RT];
   {
   const ArgPtr a = arguments();
@@ -289,7 +295,6 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
   const int G = a->G, nrows = sq.n * G;
   const uint16_t* q = a->q;
   const int64_t stride = a->q_stride;
-  const bool bf16 = a->bf16 != 0;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const int r = r0 + 16 * rt + c;
@@ -297,60 +302,55 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
     const int rr = in ? r : nrows - 1;
     node[rt] = (int32_t)pages::quotient((uint32_t)rr, group);
     const int h = kv * G + rr - node[rt] * G;
-    const uint4* src = reinterpret_cast<const uint4*>(q + (int64_t)(sq.row0 + node[rt]) * stride + (int64_t)h * kD + 32 * kg);
-    uint4 u[4];
+    const v4u* src = reinterpret_cast<const v4u*>(q + (int64_t)(sq.row0 + node[rt]) * stride + (int64_t)h * kD + 32 * kg);
+    v4u u[4];
+    float top = 0.f;
 #pragma unroll
-    for (int st = 0; st < 4; ++st) u[st] = in ? src[st] : make_uint4(0, 0, 0, 0);
-    if (bf16) {
-      // 8 significant bits are exact in fp16 from 2^-17 to 2^16 (and off by 2^-25 at most below): a row whose largest is
-      // outside [2^-4, 2^15) is scaled by a power of two that brings it to [2^14, 2^15)
-      float top = 0.f;
+    for (int st = 0; st < 4; ++st) u[st] = in ? src[st] : v4u{0, 0, 0, 0};
 #pragma unroll
-      for (int st = 0; st < 4; ++st) {
-        const uint32_t w[4] = {u[st].x, u[st].y, u[st].z, u[st].w};
+    for (int st = 0; st < 4; ++st)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(__uint_as_float(e & 1 ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16)));
+      for (int n = 0; n < 8; ++n) top = fmaxf(top, fabsf(element<BF16>(u[st][n >> 1], n & 1)));
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const int ex = top > 0.f && top < INFINITY && !(top >= 0x1p-4f && top < 0x1p5f) ? 4 - ilogbf(top) : 0;
+    if (kg == 0) sh.back[16 * rt + c] = ldexpf(1.f, -ex);
+    ranged |= __any(ex != 0);
+    v8h up;               // (-8 and -1/2: the products' sum over all dimensions is -8 sum q in every lane of the row)
+    v4f sums = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) up[e] = (_Float16)(kUp(e) ? -8.f : -0.5f);
+#pragma unroll
+    for (int st = 0; st < 4; ++st) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int n = kNib[e];
+        qb[rt][st][e] = (_Float16)ldexpf(element<BF16>(u[st][n >> 1], n & 1), kUp(e) ? ex : ex + 4);
       }
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
-      const int ex = top > 0.f && top < INFINITY && !(top >= 0x1p-4f && top < 0x1p15f) ? 14 - ilogbf(top) : 0;
-      rowf[rt] = ldexpf(1.f, -ex);
-      ranged |= __any(ex != 0);
-#pragma unroll
-      for (int st = 0; st < 4; ++st) {
-        const uint32_t w[4] = {u[st].x, u[st].y, u[st].z, u[st].w};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int n = kNib[e];
-          qb[rt][st][e] = (_Float16)ldexpf(__uint_as_float(n & 1 ? w[n >> 1] & 0xFFFF0000u : w[n >> 1] << 16), ex);
-        }
-      }
-    } else {
-      rowf[rt] = 1.f;
-#pragma unroll
-      for (int st = 0; st < 4; ++st) {
-        const v8h x = __builtin_bit_cast(v8h, u[st]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) qb[rt][st][e] = x[kNib[e]];
-      }
+      sums = __builtin_amdgcn_mfma_f32_16x16x32_f16(up, qb[rt][st], sums, 0, 0, 0);
     }
+    const float sum = sums[0];
+    const _Float16 z0 = (_Float16)sum, z1 = (_Float16)(sum - (float)z0), z2 = (_Float16)(sum - (float)z0 - (float)z1);
+    qz[rt] = kg == 0 ? v8h{z0, z1, z2, 0, 0, 0, 0, 0} : v8h{};
   }
   }
 
   float m[RT], l[RT];
-  v4f o[RT][8];
+  v4f o[RT][8], oz[RT];        // sums of weights and codes, 2^-24 their size; of weights and zero-points
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     m[rt] = kLowest;
     l[rt] = 0.f;
+    oz[rt] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) o[rt][dt] = v4f{0.f, 0.f, 0.f, 0.f};
   }
-  const Bits bits = code_bits();
   bool direct = false;         // a weight that is 0 need not mean that p is
   Stage& sg = lds.stage[wave];
   auto step = [&](int32_t t0) {
     const uint64_t there = __ballot(cur.ok);
+    // a key scale that 2^20 would take out of fp32
+    const bool large = __any(ksl > 0x1p100f);
     // ---- stage the step's scales, zero-points and value codes (a wave's LDS operations keep their order)
     {
       float v = vsl < kLeast ? kLeast : vsl;   // (NaN stays: w is NaN where it is seen)
@@ -367,14 +367,15 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
         if (zero) v = kLeast;
         direct |= __any(cur.ok && (zero || far));
       }
-      sg.ks[lane] = ksl * (0.088388347648318447f * 1.4426950408889634f);   // 1 / sqrt(128), log2 e
+      constexpr float kScore = 0.088388347648318447f * 1.4426950408889634f;   // 1 / sqrt(128), log2 e
+      sg.ks[lane] = ksl * (large ? kScore : kScore * 0x1p20f);
       sg.ls[lane] = __builtin_amdgcn_logf(v);
       sg.rs[lane] = vsl < INFINITY ? __builtin_amdgcn_rcpf(v) : 0.f; 
-      const _Float16 kzb = (_Float16)(1024.f + (float)kzl);
-      sg.kz[lane] = __builtin_bit_cast(uint32_t, v2h{kzb, kzb});
+      const uint32_t z2 = (kzl << 1) | (kzl << 17);
+      sg.kz[lane] = v4u{z2, z2, z2, z2};
       // token 16 j + 4 g + i goes to pair i of half j / 2 of lane group g, element j mod 2
       const int tj = lane >> 4, tg = (lane >> 2) & 3, ti = lane & 3;
-      sg.vz[tg * 16 + (tj >> 1) * 8 + ti * 2 + (tj & 1)] = (_Float16)((ti & 1 ? 64.f : 1024.f) + (float)vzl);
+      sg.vz[tg * 16 + (tj >> 1) * 8 + ti * 2 + (tj & 1)] = __builtin_bit_cast(_Float16, (uint16_t)vzl);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         *reinterpret_cast<uint4*>(&sg.v[(16 * j + (lane >> 2)) * (kD / 8) + 4 * ((lane & 3) ^ j)]) = vw[j];
@@ -387,29 +388,28 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
     constexpr int TJ = 4 / RT;
 #pragma unroll
     for (int j0 = 0; j0 < 4; j0 += TJ) {
-      v2h b10[TJ], b6[TJ];
       v4f acc[TJ][RT];
 #pragma unroll
       for (int j = 0; j < TJ; ++j) {
-        b10[j] = __builtin_bit_cast(v2h, sg.kz[16 * (j0 + j) + c]);
-        b6[j] = b10[j] - v2h{(_Float16)960.f, (_Float16)960.f};
+        const v8h z = __builtin_bit_cast(v8h, sg.kz[16 * (j0 + j) + c]);
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) acc[j][rt] = v4f{0.f, 0.f, 0.f, 0.f};
+        for (int rt = 0; rt < RT; ++rt) acc[j][rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(z, qz[rt], v4f{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
       }
 #pragma unroll
       for (int st = 0; st < 4; ++st)
 #pragma unroll
         for (int j = 0; j < TJ; ++j) {
           const uint4& u = kw[j0 + j];
-          const v8h kd = unpack(st == 0 ? u.x : st == 1 ? u.y : st == 2 ? u.z : u.w, bits, b10[j], b6[j], b10[j], b6[j]);
+          const v8h kd = key_codes(st == 0 ? u.x : st == 1 ? u.y : st == 2 ? u.z : u.w);
 #pragma unroll
           for (int rt = 0; rt < RT; ++rt) acc[j][rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kd, qb[rt][st], acc[j][rt], 0, 0, 0);
         }
-      if (ranged) {
+      if (ranged || large) {
+        const float f = large ? 0x1p20f : 1.f;
 #pragma unroll
         for (int j = 0; j < TJ; ++j)
 #pragma unroll
-          for (int rt = 0; rt < RT; ++rt) acc[j][rt] *= rowf[rt];
+          for (int rt = 0; rt < RT; ++rt) acc[j][rt] *= f * sh.back[16 * rt + c];
       }
 #pragma unroll
       for (int j = 0; j < TJ; ++j) {
@@ -469,20 +469,27 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
         const float mn = fmaxf(m[rt], top - kTop), f = __builtin_amdgcn_exp2f(m[rt] - mn);
         l[rt] = scaled(l[rt], m[rt] - mn);
         m[rt] = mn;
+        oz[rt] *= f;
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt) o[rt][dt] *= f;
       }
     }
     if (direct) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const v4f l4 = *reinterpret_cast<const v4f*>(&sg.ls[16 * j + 4 * kg]);
+      for (int rt = 0; rt < RT; ++rt) {
+        float base = m[rt];
+        asm volatile("" : "+v"(base));   // (or the weights below would be kept in registers from here on)
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
+        for (int j = 0; j < 4; ++j) {
+          const v4f l4 = *reinterpret_cast<const v4f*>(&sg.ls[16 * j + 4 * kg]);
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            l[rt] += y[rt][j][i] > -INFINITY && __builtin_amdgcn_exp2f(y[rt][j][i] - m[rt]) == 0.f
-                         ? __builtin_amdgcn_exp2f(y[rt][j][i] - l4[i] - m[rt]) : 0.f;
+          for (int i = 0; i < 4; ++i) {
+            const float p = __builtin_amdgcn_exp2f(y[rt][j][i] - l4[i] - base);
+            const bool lost = __builtin_amdgcn_exp2f(y[rt][j][i] - base) == 0.f, seen = y[rt][j][i] > -INFINITY;
+            l[rt] += lost & seen ? p : 0.f;
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
     }
 #pragma unroll
@@ -507,18 +514,17 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-    // ---- values: A = 16 dimensions x 32 tokens of code - z.  The transposing read hands lane (c, kg) the 16 codes of
-    // dimension 16 dt + c whose rows the 16 lanes of its group name: token 16 (c / 4) + 4 kg + c mod 4, nibble c.
+    // ---- values: A = 16 dimensions x 32 tokens of codes.  The transposing read hands lane (c, kg) the 16 codes of
+    // dimension 16 dt + c whose rows the 16 lanes of its group name: token 16 (c / 4) + 4 kg + c mod 4, nibble c.  The
+    // zero-points are one more tile, the same for all 16 of its dimensions.
     {
-      v2h bz[2][4];
-      const uint4* z4 = reinterpret_cast<const uint4*>(&sg.vz[16 * kg]);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const uint4 z = z4[h];
-        bz[h][0] = __builtin_bit_cast(v2h, z.x);
-        bz[h][1] = __builtin_bit_cast(v2h, z.y);
-        bz[h][2] = __builtin_bit_cast(v2h, z.z);
-        bz[h][3] = __builtin_bit_cast(v2h, z.w);
+        const v8h z = *reinterpret_cast<const v8h*>(&sg.vz[16 * kg + 8 * h]);
+#pragma unroll
+        for (int part = 0; part < 2; ++part)
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) oz[rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(z, part ? alo[rt][h] : ahi[rt][h], oz[rt], 0, 0, 0);
       }
       const int row = 16 * (c >> 2) + 4 * kg + (c & 3);
       constexpr int TD = 4 / RT;   // dimension tiles at a time, for four independent sums
@@ -534,7 +540,7 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
         for (int h = 0; h < 2; ++h) {
           v8h va[TD];
 #pragma unroll
-          for (int d = 0; d < TD; ++d) va[d] = unpack(h ? (uint32_t)t[d].y : (uint32_t)t[d].x, bits, bz[h][0], bz[h][1], bz[h][2], bz[h][3]);
+          for (int d = 0; d < TD; ++d) va[d] = value_codes(h ? (uint32_t)t[d].y : (uint32_t)t[d].x);
 #pragma unroll
           for (int part = 0; part < 2; ++part)
 #pragma unroll
@@ -576,7 +582,7 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
     for (int w = 1; w < kWaves; ++w) M = fmaxf(M, stat[0][w][16 * rt + c2]);
     const float f = __builtin_amdgcn_exp2f(m[rt] - M);
 #pragma unroll
-    for (int dt = 0; dt < 8; ++dt) *reinterpret_cast<v4f*>(&lds.sum[wave][c2][16 * dt + 4 * kg2]) = o[rt][dt] * f;
+    for (int dt = 0; dt < 8; ++dt) *reinterpret_cast<v4f*>(&lds.sum[wave][c2][16 * dt + 4 * kg2]) = (o[rt][dt] - oz[rt]) * (f * 0x1p24f);
     __syncthreads();
     const int row = tid >> 4, d0 = (tid & 15) * 8, r = r0 + 16 * rt + row;
     float Mr = stat[0][0][16 * rt + row], L = 0.f;
@@ -602,7 +608,7 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
         uint32_t w[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          w[e] = (uint32_t)to_bits(s[2 * e] * inv, z->bf16) | ((uint32_t)to_bits(s[2 * e + 1] * inv, z->bf16) << 16);
+          w[e] = (uint32_t)to_bits(s[2 * e] * inv, BF16) | ((uint32_t)to_bits(s[2 * e + 1] * inv, BF16) << 16);
         uint16_t* y = z->out + ((int64_t)(sq.row0 + nd) * z->Hq + kv * G + (r - nd * G)) * kD + d0;
         *reinterpret_cast<uint4*>(y) = make_uint4(w[0], w[1], w[2], w[3]);
       } else {
@@ -619,7 +625,7 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
   }
 }
 
-template <int RT>
+template <int RT, bool BF16>
 __global__ __launch_bounds__(256, 2) void k_tree(TreeArgs) {
   __shared__ __attribute__((aligned(16))) Tree<RT> sh;
   __shared__ Sequences all;
@@ -640,7 +646,7 @@ __global__ __launch_bounds__(256, 2) void k_tree(TreeArgs) {
     run.hi = pages::rounds_of(sq.len);
     run.whole = true;
     run.record = 0;
-    tree_run<RT>(sh, sq, run);
+    tree_run<RT, BF16>(sh, sq, run);
     return;
   }
   if (i >= (uint32_t)a->shares) return;
@@ -678,7 +684,7 @@ __global__ __launch_bounds__(256, 2) void k_tree(TreeArgs) {
         if (run.hi == rounds) units[1] = (int32_t)i;
       }
       if (run.r0 < sq.n * a->G) {
-        tree_run<RT>(sh, sq, run);
+        tree_run<RT, BF16>(sh, sq, run);
         __syncthreads();
       }
     }
@@ -801,7 +807,7 @@ hipError_t launch_kv4_tree(const TreeCall& t, hipStream_t s) {
   a.bf16 = t.dtype == kBF16;
   const int64_t units = ((p.shares ? p.shares : t.B * c.Hkv) + 7) / 8 * 8;
   const dim3 grid((unsigned)(units * p.blocks));
-  auto kernel = p.rt == 1 ? k_tree<1> : k_tree<2>;
+  auto kernel = p.rt == 1 ? (a.bf16 ? k_tree<1, true> : k_tree<1, false>) : a.bf16 ? k_tree<2, true> : k_tree<2, false>;
   hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.shares == 0) return e;
