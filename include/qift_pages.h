@@ -117,13 +117,13 @@ size_t qift_kv4_attention_tree_workspace_bytes(int64_t B, int32_t Hq, int32_t Hk
  *   workspace  device scratch of qift_kv4_attention_tree_workspace_bytes bytes (16-byte aligned;
  *              NULL where that is 0): partial sums of parts of long sequences.  It belongs to one call
  *              at a time: calls that overlap, two captured graphs among them, need their own.
- * Scores: fp16 products of codes and queries summed in fp32, less z times the queries' sum.  A row whose
- * largest query is outside [2^-4, 2^5) is scaled by a power of two; queries below 2^-14 (bf16: 2^-17) of a
- * scaled row, brought to [2^4, 2^5), and of bf16 rows, are off by 2^-25 at most, all others exact.  Softmax
- * statistics and sums in fp32; weights p s split into two fp16 parts (2^-21 relative).  The result is within
- * half a step of its type and (2 (S + L + 1) + 1 + lens[b] / 128) 2^-21 of the KV head's largest value, S the
- * largest |q| (|k_hat| / sqrt(128) + 2 z s) of the row and L the largest |log2| of a value scale that it
- * sees: 2e-5 at S = 16, L = 3 and 256 tokens.
+ * Scores: exact fp16 products summed in fp32.  A row whose largest query is outside [2^-4, 2^5) is scaled
+ * by a power of two that brings it to [2^4, 2^5); its queries under 2^-14 then (and a bf16 row's under 2^-17)
+ * are off by 2^-25 at most, all others exact.  Softmax statistics and sums in fp32; weights p s split into two
+ * fp16 parts (2^-21 relative).  The result is within half a step of its type and
+ * (2 (S + L + 1) + 1 + lens[b] / 96) 2^-21 of the KV head's largest value, S the largest
+ * |q| (|k_hat| / sqrt(128) + 25 s) of the row (sums of 64 + code are rounded, to nearest; 25 is reached by queries
+ * of one sign alone) and L the largest |log2| of a value scale that it sees.
  * Value scales under 2^-90 count as 2^-90.
  * B = 0 or rows = 0 does nothing.  Limits: 1 <= max_nodes <= 256, Hq a multiple of Hkv and
  * Hq / Hkv <= 64, B <= 65535, max_len < 2^28, rows < 2^31, B * Hkv * ceil(max_nodes * Hq / Hkv / 16) < 2^23.

@@ -9,12 +9,12 @@
 // sequence are joined by k_tree_merge.
 //
 // Per step, with c = lane mod 16 and kg = lane / 16:
-//   scores   D[token][row] on the f16 MFMA, A = 16 tokens x 32 dimensions of codes (exact), B = the queries, on top of -z
-//            times the row's sum of queries; lane (c, kg) receives tokens 16 j + 4 kg + i (j, i = 0 .. 3) of row c;
+//   scores   D[token][row] on the f16 MFMA, A = 16 tokens x 32 dimensions of 64 + code (exact), B = the queries, on top of
+//            -(64 + z) times the row's sum of queries; lane (c, kg) receives tokens 16 j + 4 kg + i (j, i = 0 .. 3) of row c;
 //   softmax  in the lane.  What meets the value codes is w_t = p_t s_t, so the reference m of a row is a bound of
 //            score + log2 s, not of the score: w = 2^(score + log2 s - m) then fits fp16 whatever the scales are, p = w / s
-//            goes into the sum of exponentials, and (sum w code - sum w z) / sum p is the result.  The reference only moves when
-//            it is passed by 2^8, so most steps need no reduction across lanes and no rescaling;
+//            goes into the sum of exponentials, and (sum w (64 + code) - sum w (64 + z)) / sum p is the result.  The
+//            reference only moves when it is passed by 2^8, so most steps need no reduction across lanes and no rescaling;
 //   values   D[dimension][row] += A[dimension][token] B[token][row], B = w as two fp16 parts (2^-21 relative), which the
 //            lane holds in place: the contraction's order of tokens is the one the scores left, and the transposing
 //            LDS read is given the rows of the lane's own 16 tokens, so no weight crosses lanes.
@@ -91,21 +91,27 @@ __device__ __forceinline__ int thread_again() {
   return t;
 }
 
-// Eight codes of a word as fp16 operands.  A code in the lowest bits of a half is the subnormal number code 2^-24, which the
-// matrix instructions take exactly, so no exponent is put on and no base taken off; where a code stands four bits up it is
-// 16 times that (the key side has the queries there 16 times smaller; the value side shifts, as weights would lose bits).
-// Zero-points are left out and their share is taken from the sums by one more product: the loop is bound by the instructions
-// it issues, and unpacking was the largest part of them (with an exponent and a subtraction to each pair of codes: 16 trees
-// of 64 nodes 259 us, now 246; 32 ragged sequences of one token 45, now 43).  Element e is nibble kNib[e].
+// Eight codes of a word as fp16 operands: in bits 4-7 of a half under the exponent of 64 a code is 64 + code.  The 64 and the
+// zero-point are left in, and their share is taken from the sums by one more product: the loop is bound by the
+// instructions it issues, and a subtraction to each pair of codes costs 9 instructions a word where this takes 7 (16 trees
+// of 64 nodes 258 us, now 250; chains of 5 for 16 sequences 40.1, 38.4).  Codes as subnormal numbers in a half's lowest bits
+// would take 5 (239 and 37.0), but the matrix instructions sum products of subnormals with errors up to 2^-17 of them;
+// normal ones within 2^-24, rounded to nearest, of 64 + code.  Element e is nibble kNib[e].
 constexpr int kNib[8] = {0, 4, 1, 5, 2, 6, 3, 7};
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ v8h key_codes(uint32_t w) {   // elements 2, 3, 6 and 7 (kUp) times 16
-  const uint32_t w8 = w >> 8;
-  return __builtin_bit_cast(v8h, v4u{w & 0x000F000Fu, w & 0x00F000F0u, w8 & 0x000F000Fu, w8 & 0x00F000F0u});
+// The mask and the exponent as register values the compiler knows nothing of: with literals it takes an and and an or for
+// each pair of codes, from registers the one instruction that does both.
+struct Bits {
+  uint32_t mask, e6;
+};
+__device__ __forceinline__ Bits code_bits() {
+  Bits k = {0x00F000F0u, 0x54005400u};
+  asm("" : "+s"(k.mask), "+v"(k.e6));
+  return k;
 }
-__device__ __forceinline__ constexpr bool kUp(int e) { return (e & 2) != 0; }
-__device__ __forceinline__ v8h value_codes(uint32_t w) {
-  return __builtin_bit_cast(v8h, v4u{w & 0x000F000Fu, (w >> 4) & 0x000F000Fu, (w >> 8) & 0x000F000Fu, (w >> 12) & 0x000F000Fu});
+__device__ __forceinline__ v8h unpack(uint32_t w, const Bits& k) {
+  return __builtin_bit_cast(v8h, v4u{((w << 4) & k.mask) | k.e6, (w & k.mask) | k.e6, ((w >> 4) & k.mask) | k.e6,
+                                     ((w >> 8) & k.mask) | k.e6});
 }
 
 // One of the two elements of a word of queries
@@ -144,8 +150,8 @@ struct Rows {
 struct Stage {
   uint32_t v[kStep * kD / 8];   // value codes, 64 bytes a token, 16-byte pieces of row r at piece ^ (r / 16)
   float ks[kStep], ls[kStep], rs[kStep];   // key scale log2 e / sqrt(128); log2 and reciprocal of the value scale
-  v4u kz[kStep];                // twice the key zero-point, eight times: fp16 of 2^-23 its size
-  _Float16 vz[kStep];           // value zero-point, fp16 of 2^-24 its size, in the order of use
+  v4u kz[kStep];                // an eighth of 64 + key zero-point as fp16, eight times
+  _Float16 vz[kStep];           // 64 + value zero-point, in the order of use
 };
 constexpr int kPad = kD + 4;
 union Lds {
@@ -281,10 +287,10 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
     load(cur);
   }
 
-  // ---- the queries: B operands, element e of step st is dimension 32 kg + 8 st + kNib[e] of row c, 16 times where the code
-  // is not.  fp16 holds them where the row's largest is in [2^-4, 2^5), or brought to [2^4, 2^5) by a power of two: what is
-  // below 2^-14 (bf16: 2^-17) then is off by 2^-25 at most.  What zero-points contribute, -z sum q, comes from a product of
-  // its own: -8 sum q, at most 2^15, as three fp16 parts (2^-25 off at most) in elements 0 .. 2 of lane group 0.
+  // ---- the queries: B operands, element e of step st is dimension 32 kg + 8 st + kNib[e] of row c.  A row whose largest is
+  // outside [2^-4, 2^5) is brought to [2^4, 2^5) by a power of two; what is below 2^-14 then (bf16: 2^-17) is off by 2^-25 at
+  // most.  What is to be taken off the scores, (64 + z) sum q, comes from a product of its own: -8 sum q, at most 2^15, as
+  // three fp16 parts (2^-25 off at most) in elements 0 .. 2 of lane group 0.
   v8h qb[RT][4];
   v8h qz[RT];
   bool ranged = false; // whether any row has a power of two to be taken back (sh.back; all waves write the same)
@@ -316,16 +322,16 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
     const int ex = top > 0.f && top < INFINITY && !(top >= 0x1p-4f && top < 0x1p5f) ? 4 - ilogbf(top) : 0;
     if (kg == 0) sh.back[16 * rt + c] = ldexpf(1.f, -ex);
     ranged |= __any(ex != 0);
-    v8h up;               // (-8 and -1/2: the products' sum over all dimensions is -8 sum q in every lane of the row)
+    v8h up;               // (the products' sum over all dimensions is -8 sum q in every lane of the row)
     v4f sums = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int e = 0; e < 8; ++e) up[e] = (_Float16)(kUp(e) ? -8.f : -0.5f);
+    for (int e = 0; e < 8; ++e) up[e] = (_Float16)-8.f;
 #pragma unroll
     for (int st = 0; st < 4; ++st) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const int n = kNib[e];
-        qb[rt][st][e] = (_Float16)ldexpf(element<BF16>(u[st][n >> 1], n & 1), kUp(e) ? ex : ex + 4);
+        qb[rt][st][e] = (_Float16)ldexpf(element<BF16>(u[st][n >> 1], n & 1), ex);
       }
       sums = __builtin_amdgcn_mfma_f32_16x16x32_f16(up, qb[rt][st], sums, 0, 0, 0);
     }
@@ -336,7 +342,7 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
   }
 
   float m[RT], l[RT];
-  v4f o[RT][8], oz[RT];        // sums of weights and codes, 2^-24 their size; of weights and zero-points
+  v4f o[RT][8], oz[RT];        // sums of weights times 64 + code; times 64 + zero-point
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     m[rt] = kLowest;
@@ -345,12 +351,11 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) o[rt][dt] = v4f{0.f, 0.f, 0.f, 0.f};
   }
+  const Bits bits = code_bits();
   bool direct = false;         // a weight that is 0 need not mean that p is
   Stage& sg = lds.stage[wave];
   auto step = [&](int32_t t0) {
     const uint64_t there = __ballot(cur.ok);
-    // a key scale that 2^20 would take out of fp32
-    const bool large = __any(ksl > 0x1p100f);
     // ---- stage the step's scales, zero-points and value codes (a wave's LDS operations keep their order)
     {
       float v = vsl < kLeast ? kLeast : vsl;   // (NaN stays: w is NaN where it is seen)
@@ -368,14 +373,15 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
         direct |= __any(cur.ok && (zero || far));
       }
       constexpr float kScore = 0.088388347648318447f * 1.4426950408889634f;   // 1 / sqrt(128), log2 e
-      sg.ks[lane] = ksl * (large ? kScore : kScore * 0x1p20f);
+      sg.ks[lane] = ksl * kScore;
       sg.ls[lane] = __builtin_amdgcn_logf(v);
       sg.rs[lane] = vsl < INFINITY ? __builtin_amdgcn_rcpf(v) : 0.f; 
-      const uint32_t z2 = (kzl << 1) | (kzl << 17);
+      const _Float16 zh = (_Float16)(8.f + 0.125f * (float)kzl);
+      const uint32_t z2 = __builtin_bit_cast(uint32_t, v2h{zh, zh});
       sg.kz[lane] = v4u{z2, z2, z2, z2};
       // token 16 j + 4 g + i goes to pair i of half j / 2 of lane group g, element j mod 2
       const int tj = lane >> 4, tg = (lane >> 2) & 3, ti = lane & 3;
-      sg.vz[tg * 16 + (tj >> 1) * 8 + ti * 2 + (tj & 1)] = __builtin_bit_cast(_Float16, (uint16_t)vzl);
+      sg.vz[tg * 16 + (tj >> 1) * 8 + ti * 2 + (tj & 1)] = (_Float16)(64.f + (float)vzl);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         *reinterpret_cast<uint4*>(&sg.v[(16 * j + (lane >> 2)) * (kD / 8) + 4 * ((lane & 3) ^ j)]) = vw[j];
@@ -400,16 +406,15 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
 #pragma unroll
         for (int j = 0; j < TJ; ++j) {
           const uint4& u = kw[j0 + j];
-          const v8h kd = key_codes(st == 0 ? u.x : st == 1 ? u.y : st == 2 ? u.z : u.w);
+          const v8h kd = unpack(st == 0 ? u.x : st == 1 ? u.y : st == 2 ? u.z : u.w, bits);
 #pragma unroll
           for (int rt = 0; rt < RT; ++rt) acc[j][rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kd, qb[rt][st], acc[j][rt], 0, 0, 0);
         }
-      if (ranged || large) {
-        const float f = large ? 0x1p20f : 1.f;
+      if (ranged) {
 #pragma unroll
         for (int j = 0; j < TJ; ++j)
 #pragma unroll
-          for (int rt = 0; rt < RT; ++rt) acc[j][rt] *= f * sh.back[16 * rt + c];
+          for (int rt = 0; rt < RT; ++rt) acc[j][rt] *= sh.back[16 * rt + c];
       }
 #pragma unroll
       for (int j = 0; j < TJ; ++j) {
@@ -514,7 +519,7 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-    // ---- values: A = 16 dimensions x 32 tokens of codes.  The transposing read hands lane (c, kg) the 16 codes of
+    // ---- values: A = 16 dimensions x 32 tokens of 64 + code.  The transposing read hands lane (c, kg) the 16 codes of
     // dimension 16 dt + c whose rows the 16 lanes of its group name: token 16 (c / 4) + 4 kg + c mod 4, nibble c.  The
     // zero-points are one more tile, the same for all 16 of its dimensions.
     {
@@ -540,7 +545,7 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
         for (int h = 0; h < 2; ++h) {
           v8h va[TD];
 #pragma unroll
-          for (int d = 0; d < TD; ++d) va[d] = value_codes(h ? (uint32_t)t[d].y : (uint32_t)t[d].x);
+          for (int d = 0; d < TD; ++d) va[d] = unpack(h ? (uint32_t)t[d].y : (uint32_t)t[d].x, bits);
 #pragma unroll
           for (int part = 0; part < 2; ++part)
 #pragma unroll
@@ -582,7 +587,7 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
     for (int w = 1; w < kWaves; ++w) M = fmaxf(M, stat[0][w][16 * rt + c2]);
     const float f = __builtin_amdgcn_exp2f(m[rt] - M);
 #pragma unroll
-    for (int dt = 0; dt < 8; ++dt) *reinterpret_cast<v4f*>(&lds.sum[wave][c2][16 * dt + 4 * kg2]) = (o[rt][dt] - oz[rt]) * (f * 0x1p24f);
+    for (int dt = 0; dt < 8; ++dt) *reinterpret_cast<v4f*>(&lds.sum[wave][c2][16 * dt + 4 * kg2]) = (o[rt][dt] - oz[rt]) * f;
     __syncthreads();
     const int row = tid >> 4, d0 = (tid & 15) * 8, r = r0 + 16 * rt + row;
     float Mr = stat[0][0][16 * rt + row], L = 0.f;

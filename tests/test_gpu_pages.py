@@ -7,8 +7,9 @@ values s (q - z) have one rounding from fp32, which is the same on both sides to
 Attention, per query head, against fp64 on the same cache: |y - ref| <= h |ref| + e, h the half step of the output's type
 (fp16 2^-11, bf16 2^-8; and 2^-25 for fp16 outputs below the normal numbers) and e the arithmetic's part:
   scores are sums of 128 exact products in fp32 (the MFMA's sums are within 2^-22 of the sum of |products|, which is at
-  most S = |q| |k| / sqrt(128) for the score where zero-points are taken off the codes first; taken off the sum, 2 z s |q|
-  more, which the rounding errors' random signs stay under, so the limit is left without it); the scale, the factor to powers of two and log2 of the value's scale
+  most S = |q| |k| / sqrt(128) for the score where zero-points are taken off the codes first; where 64 + z is taken off
+  sums of 64 + code, five roundings of partial sums of about 64 |q| s, (5 / 16) 7 |q| s 2^-21, which stays under S of
+  keys that fill their codes, |k| about 4 s sqrt(128)); the scale, the factor to powers of two and log2 of the value's scale
   (L the largest |log2 s|) each round once more, as do the logarithm, the exponential and the reciprocal: in all a
   weight is off by at most (S + L) 2^-21 + 2^-21 relative, and the output by twice that times max |v|;
   weights are held to 2^-21, and sums of T / 32 matrix instructions in fp32: (2^-21 + T / 32 * 2^-24) max |v|.
