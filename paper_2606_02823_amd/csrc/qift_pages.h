@@ -118,6 +118,16 @@ inline Plan plan(int64_t B, int32_t Hkv, int32_t G, int32_t max_nodes, int64_t m
 // rounds round_at(lo) .. round_at(hi) - 1, if any.
 QIFT_HD int32_t slots_of(int32_t len) { return rounds_of(len) + kBegin; }
 QIFT_HD int32_t used_shares(int64_t W, int32_t shares) { return W < shares ? (int32_t)W : shares; }
+// The share and block of rows of workgroup g: group g is on XCD g mod 8, which has every eighth part, in order, of the shares'
+// blocks.  A share past the last one: the workgroup has none.
+struct Place {
+  int32_t share, block;
+};
+QIFT_HD Place place(int32_t g, int32_t shares, int32_t blocks) {
+  const int32_t all = shares * blocks, per = (all + 7) / 8, j = g / 8, n = g % 8 * per + j;
+  if (j >= per || n >= all) return {shares, 0};
+  return {n / blocks, n % blocks};
+}
 QIFT_HD int64_t first_slot(int64_t W, int32_t n, int32_t i) { return W * i / n; }
 QIFT_HD int32_t round_at(int32_t slot) { return slot > kBegin ? slot - kBegin : 0; }
 // Partial records: share i and unit u have number i + u (both grow along the rounds, so no two have the same), each

@@ -651,12 +651,13 @@ __global__ __launch_bounds__(256, 2) void k_tree(TreeArgs) {
   __shared__ __attribute__((aligned(16))) Tree<RT> sh;
   __shared__ Sequences all;
   const ArgPtr a = arguments();
-  // blocks of rows over the same tokens are 8 workgroups apart: one XCD, whose L2 then holds the tokens
-  const uint32_t per = 8u * (uint32_t)a->blocks;
-  const uint32_t i = (blockIdx.x / per) * 8 + blockIdx.x % 8, block = (blockIdx.x % per) / 8;
+  // Workgroups go to the XCDs in turn.  Blocks of rows over the same tokens are taken by one XCD, whose L2 then holds the
+  // tokens.
   Run run;
-  run.r0 = (int)block * 16 * RT;
   if (a->shares == 0) {
+    const uint32_t per = 8u * (uint32_t)a->blocks;
+    const uint32_t i = (blockIdx.x / per) * 8 + blockIdx.x % 8, block = (blockIdx.x % per) / 8;
+    run.r0 = (int)block * 16 * RT;
     run.b = (int)(i / (uint32_t)a->Hkv);
     run.kv = (int)(i % (uint32_t)a->Hkv);
     if (run.b >= a->B) return;
@@ -670,14 +671,19 @@ __global__ __launch_bounds__(256, 2) void k_tree(TreeArgs) {
     tree_run<RT, BF16>(sh, sq, run);
     return;
   }
-  if (i >= (uint32_t)a->shares) return;
   add_slots(a, all, blockIdx.x == 0);
   const int B = a->B, Hkv = a->Hkv;
   const int64_t W = (int64_t)uniform(all.before[B]) * Hkv;
+  // An XCD has an eighth of all blocks of all shares, one share's blocks after another's: as many as it has room for, so that
+  // none waits for another to end (4 sequences of 69 nodes and 2984 tokens, 16 heads a group, 35 blocks and 14 shares: 48
+  // us; with whole shares to an XCD, some with two and some with one, 65).
   const int32_t shares = pages::used_shares(W, a->shares);
-  if ((int32_t)i >= shares) return;
-  int64_t pos = pages::first_slot(W, shares, (int32_t)i);
-  const int64_t stop = pages::first_slot(W, shares, (int32_t)i + 1);
+  const pages::Place mine = pages::place((int32_t)blockIdx.x, shares, a->blocks);
+  if (mine.share >= shares) return;
+  const int32_t i = mine.share, block = mine.block;
+  run.r0 = block * 16 * RT;
+  int64_t pos = pages::first_slot(W, shares, i);
+  const int64_t stop = pages::first_slot(W, shares, i + 1);
   // the sequence of the share's first slot: as many as have all their slots before it (those without slots too)
   int b = 0;
   for (int b0 = 0; b0 < B; b0 += 64) {
@@ -701,8 +707,8 @@ __global__ __launch_bounds__(256, 2) void k_tree(TreeArgs) {
       run.record = (int64_t)i + (int64_t)b * Hkv + run.kv;
       if (block == 0 && threadIdx.x == 0) {   // which shares have the unit, for k_tree_merge
         int32_t* units = reinterpret_cast<int32_t*>(a->part + a->records * (kD + 2)) + 2 * ((int64_t)b * Hkv + run.kv);
-        if (run.lo == 0) units[0] = (int32_t)i;
-        if (run.hi == rounds) units[1] = (int32_t)i;
+        if (run.lo == 0) units[0] = i;
+        if (run.hi == rounds) units[1] = i;
       }
       if (run.r0 < sq.n * a->G) {
         tree_run<RT, BF16>(sh, sq, run);
@@ -826,8 +832,8 @@ hipError_t launch_kv4_tree(const TreeCall& t, hipStream_t s) {
   a.shares = p.shares;
   a.blocks = p.blocks;
   a.bf16 = t.dtype == kBF16;
-  const int64_t units = ((p.shares ? p.shares : t.B * c.Hkv) + 7) / 8 * 8;
-  const dim3 grid((unsigned)(units * p.blocks));
+  const int64_t groups = p.shares ? ((int64_t)p.shares * p.blocks + 7) / 8 * 8 : (t.B * c.Hkv + 7) / 8 * 8 * p.blocks;
+  const dim3 grid((unsigned)groups);
   auto kernel = p.rt == 1 ? (a.bf16 ? k_tree<1, true> : k_tree<1, false>) : a.bf16 ? k_tree<2, true> : k_tree<2, false>;
   hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a);
   hipError_t e = hipGetLastError();

@@ -76,6 +76,11 @@ int main() {
       int len;
       std::scanf("%d", &len);
       std::printf("%d %d\n", rounds_of(len), slots_of(len));
+    } else if (!std::strcmp(what, "place")) {
+      int g, shares, blocks;
+      std::scanf("%d %d %d", &g, &shares, &blocks);
+      const Place p = place(g, shares, blocks);
+      std::printf("%d %d\n", p.share, p.block);
     } else if (!std::strcmp(what, "round")) {
       int slot;
       std::scanf("%d", &slot);
@@ -200,6 +205,22 @@ def test_plan_covers_every_row(ask):
         assert rt in (1, 2, 4) and blocks * 16 * rt >= nodes * G > (blocks - 1) * 16 * rt
         assert 0 <= shares <= B * Hkv * (-(-length // 256) + 2) and (B <= 512 or shares == 0)
         assert records == (shares + B * Hkv if shares else 0)
+
+
+def test_every_block_of_every_share_has_one_workgroup(ask):
+    """Also where fewer shares are used than the launch was made for; and no XCD (every eighth workgroup) has more than
+    its part."""
+    rng = np.random.default_rng(12)
+    for _ in range(60):
+        blocks = int(np.exp(rng.uniform(0, 6.9)))
+        planned = max(1, 512 // blocks)
+        used = planned if rng.integers(0, 2) else int(rng.integers(0, planned + 1))
+        groups = (planned * blocks + 7) // 8 * 8
+        got = ask([("place", g, used, blocks) for g in range(groups)])
+        at = [(g, s, k) for g, (s, k) in enumerate(got) if s < used]
+        assert all(s >= 0 and 0 <= k < blocks for _, s, k in at)
+        assert sorted((s, k) for _, s, k in at) == [(s, k) for s in range(used) for k in range(blocks)]
+        assert max([sum(g % 8 == x for g, _, _ in at) for x in range(8)]) == -(-used * blocks // 8)
 
 
 def test_shares_cover_every_round_once(ask):
