@@ -90,10 +90,15 @@ QIFT_HD uint64_t tree_bits(int32_t d0, uint64_t w0, uint64_t w1) {
 // waves.  Few units: the rounds of all units, in order, are dealt out evenly to `shares` workgroups a block of rows, whatever the
 // sequences' lengths are; a unit that more than one share covers is joined from partial records.  Beginning and ending a
 // unit takes a workgroup longer than a round, so a unit is dealt out as its rounds and kBegin more before them (32
-// ragged sequences of 8 heads, where a share may have eight short units: 52 us with 0, 46 with 1, 45 with 2).  Many units: one workgroup takes a unit whole.
+// ragged sequences of 8 heads, where a share may have eight short units: 52 us with 0, 46 with 1, 45 with 2).
+// Many units: one workgroup takes a unit whole, which needs no second launch.  With two workgroups to a CU's place or more
+// (16 trees of 64 nodes over 8192 tokens, 1024 blocks of units: 257 us, dealt out 269; 4 ragged chunks of 256: 61, 67), and
+// with half of the places filled where sequences have few rounds (256 blocks, 673 tokens: 17 us, dealt out 24; 448, 1021
+// tokens: 29, 40; 480, 332 tokens: 25, 29).  Below that dealing out wins (256 units of 32 ragged sequences of up to 8192
+// tokens: 45 us, whole 70; 280 blocks, 2999 tokens: 36.5, 38).
 constexpr int kStep = 64, kWaves = 4, kRound = kStep * kWaves;
 constexpr int kMostShared = 512;   // sequences whose rounds are dealt out (every workgroup adds them up)
-constexpr int kBegin = 2;
+constexpr int kBegin = 2, kFewRounds = 4;
 struct Plan {
   int32_t rt, blocks;   // row tiles of a workgroup, blocks of a KV head's rows
   int32_t shares;       // workgroups of a block of rows; 0: one to a unit
@@ -106,7 +111,7 @@ inline Plan plan(int64_t B, int32_t Hkv, int32_t G, int32_t max_nodes, int64_t m
   p.blocks = (int32_t)((rows + 16 * p.rt - 1) / (16 * p.rt));
   const int64_t units = B * Hkv, rounds = (max_len + kRound - 1) / kRound;
   p.shares = 0;
-  if (rounds > 1 && B <= kMostShared && units * p.blocks < 1024) {
+  if (rounds > 1 && B <= kMostShared && units * p.blocks < (rounds <= kFewRounds ? 256 : 1024)) {
     int64_t n = 512 / p.blocks;                 // two workgroups to each of 256 CUs
     if (n > units * (rounds + kBegin)) n = units * (rounds + kBegin);
     p.shares = n < 1 ? 1 : (int32_t)n;
