@@ -311,6 +311,22 @@ def test_sharp_scores(Q, dtype):
     c.check(c.run(Q), "sharp")
 
 
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16], ids=["fp16", "bf16"])
+def test_queries_of_every_size(Q, dtype):
+    """Rows far below and above 1, some of one value alone and some of one sign, among ordinary ones."""
+    rng = np.random.default_rng(7)
+    for n, t in ((1, 300), (12, 700), (40, 1500)):
+        c = Case(Q, 110 + n, [(n, t)], 16, 4, 64, dtype)
+        size = 10.0 ** rng.uniform(-6 if dtype == torch.float16 else -30, 2, (n, 16, 1))
+        size[::3] = 1.0
+        q = values(c.q) * size
+        q[:, 3, 1:] = 0.0
+        q[:, 7] = np.abs(q[:, 7])
+        q[:, 11] = 0.0
+        c.q = torch.from_numpy(q).to(dtype)
+        c.check(c.run(Q), f"{n} rows of any size")
+
+
 @pytest.mark.parametrize("vscale", [1e-6, 3e3])
 def test_scale_of_the_values(Q, vscale):
     for dtype in (torch.float16, torch.bfloat16):
@@ -352,7 +368,10 @@ def test_many_sequences_of_any_length(Q):
     c = Case(Q, 98, seqs, 4, 1, 16, torch.bfloat16)
     c.check(c.run(Q), "a workgroup each")
     c = Case(Q, 99, seqs[:510], 4, 1, 16, torch.bfloat16)
-    c.check(c.run(Q), "dealt out")
+    c.check(c.run(Q), "short, a workgroup each")
+    c.check(c.run(Q, max_len=2000), "short, dealt out")
+    c = Case(Q, 102, seqs[:400] + [(3, 1700)], 4, 1, 16, torch.float16)
+    c.check(c.run(Q), "one long, dealt out")
     assert Q.device_error() == 0
 
 
