@@ -459,6 +459,13 @@ def _empty(shape, dtype, device, stream=None) -> torch.Tensor:
         return torch.empty(shape, dtype=dtype, device=device)
 
 
+def _empty_pair(shape, dtype, device, stream=None):
+    if stream is None:
+        a = torch.empty(shape, dtype=dtype, device=device)
+        return a, torch.empty_like(a)   # (0.5 us less than another torch.empty)
+    return _empty(shape, dtype, device, stream), _empty(shape, dtype, device, stream)
+
+
 _HALVES = (torch.float16, torch.bfloat16)
 
 
@@ -513,7 +520,7 @@ def kv4_append(cache: KV4Pages, k: torch.Tensor, v: torch.Tensor, slots: torch.T
     ks, vs = _rows(k, index, dt, shape, "k"), _rows(v, index, dt, shape, "v")
     _dense(slots, index, torch.int32, (n,), "slots")
     if values is True:
-        ko, vo = _empty(shape, dt, cache.device, stream), _empty(shape, dt, cache.device, stream)
+        ko, vo = _empty_pair(shape, dt, cache.device, stream)
     elif values is False or values is None:
         ko = vo = None
     else:
@@ -535,7 +542,7 @@ def kv4_read(cache: KV4Pages, slots: torch.Tensor, dtype=torch.float16, out=None
     _dense(slots, index, torch.int32, (n,), "slots")
     shape = (n, cache.Hkv, 128)
     if out is None:
-        ko, vo = _empty(shape, dtype, cache.device, stream), _empty(shape, dtype, cache.device, stream)
+        ko, vo = _empty_pair(shape, dtype, cache.device, stream)
     else:
         ko, vo = out
         _dense(ko, index, dtype, shape, "out")
@@ -579,12 +586,14 @@ def kv4_attention_tree(q: torch.Tensor, cache: KV4Pages, table: torch.Tensor, st
         _dense(out, index, dt, shape, "out")
     if workspace is None:
         need = int(lib().qift_kv4_attention_tree_workspace_bytes(B, Hq, cache.Hkv, 128, max_nodes, max_len))
-        workspace = _empty((max(need, 16),), torch.uint8, cache.device, stream)
+        if need:
+            workspace = _empty((need,), torch.uint8, cache.device, stream)
     else:
         _dense(workspace, index, torch.uint8, (workspace.numel(),), "workspace")
+        need = workspace.numel()
     st = _run(index, lib().qift_kv4_attention_tree,
               (cache._ref, q.data_ptr(), qs, _DTYPE[dt], rows, table.data_ptr(), pages, starts.data_ptr(), lens.data_ptr(), B,
-               Hq, max_nodes, max_len, _ptr(visible), out.data_ptr(), workspace.data_ptr(), workspace.numel()), stream)
+               Hq, max_nodes, max_len, _ptr(visible), out.data_ptr(), _ptr(workspace), need), stream)
     if st:
         _check("qift_kv4_attention_tree", st)
     return out
