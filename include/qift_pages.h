@@ -105,8 +105,10 @@ size_t qift_kv4_attention_tree_workspace_bytes(int64_t B, int32_t Hq, int32_t Hk
  *   rows       rows of q and out; rows at or past starts[B] of out are left as they were.
  *   table      int32 [B][table_pages]; only the entries that positions below lens[b] need are read.
  *              An entry outside [0, pages): its positions are not seen, QIFT_DEVERR_INDEX.
- *   starts     int32 [B + 1], ascending from 0.  Rows outside [0, rows) and nodes past max_nodes are
- *              not computed, QIFT_DEVERR_INDEX.
+ *   starts     int32 [B + 1], ascending from 0.  A sequence's nodes past max_nodes, and those at or past
+ *              row `rows`, are left out, QIFT_DEVERR_INDEX: not computed and, whatever a mask says, not
+ *              seen; its other nodes keep their places.  A sequence whose first row is outside [0, rows]
+ *              has none of its rows computed, QIFT_DEVERR_INDEX.
  *   lens       int32 [B], n_b <= lens[b] <= max_len and lens[b] <= table_pages * page.  A length
  *              outside [0, that limit] is taken as the nearer end, QIFT_DEVERR_INDEX; for lens[b] < n_b
  *              the nodes past lens[b] have no position and are not seen.

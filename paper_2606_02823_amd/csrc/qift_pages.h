@@ -43,23 +43,25 @@ QIFT_HD uint32_t token_row(uint32_t t, uint32_t entry, uint32_t Hkv, uint32_t he
 }
 
 // Nodes and tokens of one sequence, taken from device data that may hold anything: every count is brought into the
-// range the launch was made for, and bad says that one was not.
+// range the launch was made for, and bad says that one was not.  The nodes stand where the starts put them: those past
+// max_nodes or past the last row are left out with their tokens, which lie behind the others', and the others keep their
+// places.  A sequence whose first row is none has no rows.
 struct Seq {
   int32_t row0, n, len, ctx;   // first row of q, rows, cached tokens, tokens before the first node
   bool bad;
 };
 QIFT_HD Seq sequence(int32_t s0, int32_t s1, int32_t len, int32_t rows, int32_t max_nodes, int64_t most) {
   Seq q;
-  q.bad = s0 < 0 || s1 < s0 || s1 > rows || len < 0 || (int64_t)len > most;
-  q.row0 = s0 < 0 ? 0 : s0 > rows ? rows : s0;
-  const int32_t end = s1 < q.row0 ? q.row0 : s1 > rows ? rows : s1;
-  q.n = end - q.row0;
-  if (q.n > max_nodes) {
-    q.n = max_nodes;
-    q.bad = true;
-  }
+  const int64_t nodes = s1 < s0 ? 0 : (int64_t)s1 - s0;
+  const bool none = s0 < 0 || s0 > rows;
+  q.bad = none || s1 < s0 || s1 > rows || nodes > max_nodes || len < 0 || (int64_t)len > most;
+  q.row0 = none ? 0 : s0;
+  q.n = none ? 0 : rows - s0;
+  if (q.n > max_nodes) q.n = max_nodes;
+  if (q.n > nodes) q.n = (int32_t)nodes;
   q.len = len < 0 ? 0 : (int64_t)len > most ? (int32_t)most : len;
-  q.ctx = q.len > q.n ? q.len - q.n : 0;
+  q.ctx = q.len > nodes ? q.len - (int32_t)nodes : 0;
+  if (nodes > q.n && q.len > q.ctx + q.n) q.len = q.ctx + q.n;
   return q;
 }
 

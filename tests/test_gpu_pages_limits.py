@@ -1,0 +1,68 @@
+"""The paged KV4 cache at its limits: counts and rows past what a call was made for, scores at the ends of fp32's range,
+long sums, and the forms of the calls that take their outputs."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import pages as opages
+from test_gpu_pages import HALF, Case, Q, random_tree, tensor, values   # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def near(c, got, ref, b, lead=""):
+    """Rows of sequence b against fp64, within the limit that test_gpu_pages derives (its own formula, for some rows)."""
+    n, t = len(got), c.seqs[b][1]
+    q = values(c.q[c.starts[b]:c.starts[b] + n]).astype(np.float64)
+    G = c.Hq // c.Hkv
+    kn = np.linalg.norm(c.k[b].astype(np.float64), axis=-1).max(axis=0)
+    vmax = np.abs(c.v[b]).max(axis=(0, 2))
+    S = np.linalg.norm(q, axis=-1) * np.repeat(kn, G)[None] / np.sqrt(128.0)
+    L = np.abs(np.log2(np.maximum(c.scales[b], 2.0 ** -90))).max()
+    e = (2 * (S + L + 1) * 2.0 ** -21 + 2.0 ** -21 + t / 32 * 2.0 ** -24) * np.repeat(vmax, G)[None]
+    if c.dtype == torch.float16:
+        e = e + 2.0 ** -25
+    over = np.abs(values(got).astype(np.float64) - ref) / (HALF[c.dtype] * np.abs(ref) + e[..., None])
+    assert over.max() <= 1.0, (lead, b, float(over.max()))
+
+
+@pytest.mark.parametrize("masked", [False, True], ids=["chain", "tree"])
+def test_first_nodes_of_sequences_with_too_many(Q, masked):  # noqa: F811
+    """The nodes that a call was made for keep their places when a sequence has more, or when q has fewer rows than the
+    starts say; those left out are neither computed nor seen, and the error word says so."""
+    rng = np.random.default_rng(11)
+    seqs = [(3, 400), (9, 1300)]
+    masks = [random_tree(rng, n) for n, _ in seqs] if masked else None
+    c = Case(Q, 120, seqs, 16, 4, 32, torch.float16, masks)
+    ref = [c.reference(b) for b in range(2)]
+    if masked:                                   # rows that name a node that is left out do not see it
+        for m in masks:
+            m[:2, 2] = True
+    assert Q.device_error() == 0
+    out = torch.full((c.rows, 16, 128), 7.0, dtype=torch.float16, device="cuda")
+    for most_len in (1300, 5000):
+        out.fill_(7.0)
+        y = c.run(Q, max_nodes=2, max_len=most_len, out=out)
+        assert Q.device_error() == Q.DEVERR_INDEX
+        for b in range(2):
+            s = c.starts[b]
+            near(c, y[s:s + 2], ref[b][:2], b, "two nodes")
+            assert (y[s + 2:c.starts[b + 1]] == 7.0).all()
+    # two rows fewer than the starts say: the last sequence loses its last two nodes
+    visible = c.visible(9)
+    if masked:
+        for m in masks:
+            m[:2, 2] = False
+        visible = c.visible(9)
+        visible[c.starts[1]:, 0] |= 1 << 7
+    y = Q.kv4_attention_tree(c.q[:-2].cuda(), c.cache, tensor(c.table), tensor(c.starts), tensor(c.lens), max_nodes=9, max_len=1300,
+                             visible=None if visible is None else visible[:-2].contiguous())
+    assert Q.device_error() == Q.DEVERR_INDEX
+    near(c, y[:3], ref[0], 0)
+    near(c, y[3:], ref[1][:7], 1, "seven rows")
+    # a first row that is none: the sequence has no rows
+    out.fill_(7.0)
+    Q.kv4_attention_tree(c.q.cuda(), c.cache, tensor(c.table), tensor(np.array([-4, 3, 12], dtype=np.int32)), tensor(c.lens),
+                         max_nodes=9, max_len=1300, visible=visible, out=out)
+    assert Q.device_error() == Q.DEVERR_INDEX
+    assert (out[:3] == 7.0).all()

@@ -407,3 +407,25 @@ def test_oracle_append_then_read():
     assert not values[2].any() and not values[4].any()                 # padding, and past the pool
     assert (after[1] != 0).sum() == 4 * Hkv
     assert np.abs(values[0] - x[0]).max() <= after[1].max() * 4        # within the clipped range's steps
+
+
+def test_nodes_that_are_left_out_do_not_move_the_others(ask):
+    """A sequence with more nodes than the launch was made for, or than there are rows: the first ones stand where the
+    starts and the length put them, and the tokens of the others, which come behind, are cut off.  A sequence whose first
+    row is none has no rows at all."""
+    rng = np.random.default_rng(13)
+    lines = [("seq", 0, 3, 400, 3, 2, 1000), ("seq", 0, 3, 400, 2, 256, 1000), ("seq", 0, 5, 3, 5, 2, 1000),
+             ("seq", -4, 3, 400, 5, 256, 1000), ("seq", 6, 9, 400, 5, 256, 1000), ("seq", 0, 2 ** 31 - 1, 400, 5, 256, 1000)]
+    got = ask(lines)
+    assert got[:2] == [[0, 2, 399, 397, 1]] * 2 and got[2] == [0, 2, 2, 0, 1]
+    assert got[3][1] == got[4][1] == 0 and got[5] == [0, 5, 5, 0, 1]
+    lines = []
+    for _ in range(3000):
+        rows = int(rng.integers(1, 40))
+        s0 = int(rng.integers(0, rows + 1))
+        lines.append(("seq", s0, s0 + int(rng.integers(0, 60)), int(rng.integers(0, 200)), rows, int(rng.integers(1, 50)), 150))
+    for (_, s0, s1, ln, rows, most_nodes, most), (row0, n, length, ctx, bad) in zip(lines, ask(lines)):
+        nodes, ln = s1 - s0, min(ln, most)
+        assert row0 == s0 and n == min(nodes, rows - s0, most_nodes)
+        assert ctx == max(0, ln - nodes)
+        assert length == (ln if n == nodes else min(ln, ctx + n))
