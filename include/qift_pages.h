@@ -126,7 +126,8 @@ size_t qift_kv4_attention_tree_workspace_bytes(int64_t B, int32_t Hq, int32_t Hk
  * (2 (S + L + 1) + 1 + lens[b] / 96) 2^-21 of the KV head's largest value, S the largest
  * |q| (|k_hat| / sqrt(128) + 25 s) of the row (sums of 64 + code are rounded, to nearest; 25 is reached by queries
  * of one sign alone) and L the largest |log2| of a value scale that it sees.
- * Value scales under 2^-90 count as 2^-90.
+ * Value scales under 2^-90 count as 2^-90.  A score that with log2 of its value's scale, both as powers of
+ * two, is past fp32's lowest value counts as not seen; past its largest, the row is NaN.
  * B = 0 or rows = 0 does nothing.  Limits: 1 <= max_nodes <= 256, Hq a multiple of Hkv and
  * Hq / Hkv <= 64, B <= 65535, max_len < 2^28, rows < 2^31, B * Hkv * ceil(max_nodes * Hq / Hkv / 16) < 2^23.
  * Up to two launches.

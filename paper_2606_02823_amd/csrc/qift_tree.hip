@@ -34,7 +34,7 @@ typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef int v2i __attribute__((ext_vector_type(2)));
 
-constexpr float kLowest = -0x1p127f;   // the reference of a row that has seen nothing: finite, below the scores of any queries
+constexpr float kLowest = -0x1.fffffep127f;   // the reference of a row that has seen nothing: no finite score is below it
 constexpr float kSlack = 8.f;       // how far, as a power of two, a weight may pass 1 before the reference moves
 constexpr float kTop = 7.f;         // w at the reference is 2^kTop, so w < 2^(kSlack + kTop) = 2^15
 // A vector of zeros has scale 1 whatever the scales around it, so kLeast stands for it in the reference (and for smaller

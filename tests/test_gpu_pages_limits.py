@@ -66,3 +66,20 @@ def test_first_nodes_of_sequences_with_too_many(Q, masked):  # noqa: F811
                          max_nodes=9, max_len=1300, visible=visible, out=out)
     assert Q.device_error() == Q.DEVERR_INDEX
     assert (out[:3] == 7.0).all()
+
+
+def test_scores_at_the_ends_of_fp32(Q):  # noqa: F811
+    """One seen token is the whole softmax while its score is finite in fp32: scores (in powers of two, as the kernel has
+    them) between -2^128 and -2^127, or 2^127 and 2^128."""
+    only = np.array([[False, True], [False, True]])
+    for kscale, top in ((300.0, 2.9e38),):
+        c = Case(Q, 121, [(2, 2)] * 6, 8, 2, 16, torch.bfloat16, [only] * 6, kscale=kscale)
+        pick = lambda x: torch.from_numpy(np.stack([t[1] for t in x for _ in range(2)])).repeat_interleave(4, dim=1)  # noqa: E731
+        key, ref = pick(c.k), pick(c.v)
+        norm = (key.double() ** 2).sum(-1, keepdim=True)
+        for sign in (-1.0, 1.0):
+            # a score of sign * top in powers of two, before log2 of the value's scale (a few)
+            c.q = (sign * top * np.sqrt(128.0) / np.log2(np.e) / norm * key).to(torch.bfloat16)
+            assert torch.isfinite(c.q.float()).all()
+            y = c.run(Q).float().cpu()
+            assert (y - ref).abs().le(ref.abs() * (2.0 ** -8 + 2.0 ** -20)).all(), (kscale, sign)
