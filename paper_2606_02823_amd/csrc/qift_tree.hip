@@ -415,20 +415,23 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
       for (int j = 0; j < TJ; ++j)
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) acc[j][rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(z[j], qz[rt], acc[j][rt], 0, 0, 0);
-      if (ranged) {
-#pragma unroll
-        for (int j = 0; j < TJ; ++j)
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt) acc[j][rt] *= sh.back[16 * rt + c];
-      }
 #pragma unroll
       for (int j = 0; j < TJ; ++j) {
         const v4f k4 = *reinterpret_cast<const v4f*>(&sg.ks[16 * (j0 + j) + 4 * kg]);
         const v4f l4 = *reinterpret_cast<const v4f*>(&sg.ls[16 * (j0 + j) + 4 * kg]);
+        if (ranged) {   // a power of two below 1 goes to the sums, one above 1 comes after the key's scale: no product leaves fp32 before the score does
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
+          for (int rt = 0; rt < RT; ++rt) {
+            const float back = sh.back[16 * rt + c], down = fminf(back, 1.f), up = fmaxf(back, 1.f);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) y[rt][j0 + j][i] = fmaf(acc[j][rt][i], k4[i], l4[i]);
+            for (int i = 0; i < 4; ++i) y[rt][j0 + j][i] = fmaf(acc[j][rt][i] * down * k4[i], up, l4[i]);
+          }
+        } else {
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[rt][j0 + j][i] = fmaf(acc[j][rt][i], k4[i], l4[i]);
+        }
       }
       __builtin_amdgcn_sched_barrier(0);
     }

@@ -70,9 +70,9 @@ def test_first_nodes_of_sequences_with_too_many(Q, masked):  # noqa: F811
 
 def test_scores_at_the_ends_of_fp32(Q):  # noqa: F811
     """One seen token is the whole softmax while its score is finite in fp32: scores (in powers of two, as the kernel has
-    them) between -2^128 and -2^127, or 2^127 and 2^128."""
+    them) between -2^128 and -2^127, and scores whose sum of products before the key's scale is past fp32."""
     only = np.array([[False, True], [False, True]])
-    for kscale, top in ((300.0, 2.9e38),):
+    for kscale, top in ((300.0, 2.9e38), (1.0, 5e37), (1e-3, 1e36)):
         c = Case(Q, 121, [(2, 2)] * 6, 8, 2, 16, torch.bfloat16, [only] * 6, kscale=kscale)
         pick = lambda x: torch.from_numpy(np.stack([t[1] for t in x for _ in range(2)])).repeat_interleave(4, dim=1)  # noqa: E731
         key, ref = pick(c.k), pick(c.v)
