@@ -9,12 +9,12 @@
 // sequence are joined by k_tree_merge.
 //
 // Per step, with c = lane mod 16 and kg = lane / 16:
-//   scores   D[token][row] on the f16 MFMA, A = 16 tokens x 32 dimensions of 64 + code (exact), B = the queries, on top of
-//            -(64 + z) times the row's sum of queries; lane (c, kg) receives tokens 16 j + 4 kg + i (j, i = 0 .. 3) of row c;
+//   scores   D[token][row] on the f16 MFMA, A = 16 tokens x 32 dimensions of code - z (exact), B = the queries; lane
+//            (c, kg) receives tokens 16 j + 4 kg + i (j, i = 0 .. 3) of row c;
 //   softmax  in the lane.  What meets the value codes is w_t = p_t s_t, so the reference m of a row is a bound of
 //            score + log2 s, not of the score: w = 2^(score + log2 s - m) then fits fp16 whatever the scales are, p = w / s
-//            goes into the sum of exponentials, and (sum w (64 + code) - sum w (64 + z)) / sum p is the result.  The
-//            reference only moves when it is passed by 2^8, so most steps need no reduction across lanes and no rescaling;
+//            goes into the sum of exponentials, and sum w (code - z) / sum p is the result.  The reference only moves when
+//            it is passed by 2^8, so most steps need no reduction across lanes and no rescaling;
 //   values   D[dimension][row] += A[dimension][token] B[token][row], B = w as two fp16 parts (2^-21 relative), which the
 //            lane holds in place: the contraction's order of tokens is the one the scores left, and the transposing
 //            LDS read is given the rows of the lane's own 16 tokens, so no weight crosses lanes.
@@ -33,6 +33,8 @@ using pages::kWaves;
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef int v2i __attribute__((ext_vector_type(2)));
+typedef _Float16 v4h __attribute__((ext_vector_type(4)));
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 
 constexpr float kLowest = -0x1.fffffep127f;   // the reference of a row that has seen nothing: no finite score is below it
 constexpr float kSlack = 8.f;       // how far, as a power of two, a weight may pass 1 before the reference moves
@@ -91,27 +93,32 @@ __device__ __forceinline__ int thread_again() {
   return t;
 }
 
-// Eight codes of a word as fp16 operands: in bits 4-7 of a half under the exponent of 64 a code is 64 + code.  The 64 and the
-// zero-point are left in, and their share is taken from the sums by one more product: the loop is bound by the
-// instructions it issues, and a subtraction to each pair of codes costs 9 instructions a word where this takes 7 (16 trees
-// of 64 nodes 258 us, now 250; chains of 5 for 16 sequences 40.1, 38.4).  Codes as subnormal numbers in a half's lowest bits
-// would take 5 (239 and 37.0), but the matrix instructions sum products of subnormals with errors up to 2^-17 of them;
-// normal ones within 2^-24, rounded to nearest, of 64 + code.  Element e is nibble kNib[e].
+// Eight codes of a word less their zero-points, as exact fp16 operands: a code in bits 0-3 of a half under the exponent of
+// 1024 is 1024 + code, one in bits 4-7 under that of 64 is 64 + code; then the base, 1024 or 64 plus the zero-point (exact for
+// every byte), is subtracted.  Left in the operands, with its share taken from the sums by one more product, the base would
+// save two of these nine instructions a word (16 trees of 64 nodes 264 us, then 255; chains of 5 for 16 sequences 37.3, 35.9;
+// 32 ragged sequences 43.9, 42.0), but the sums would be of 64 to 79 times the weights and round as such: up to 2^-9 of the
+// largest value was lost so over 65536 tokens whose first have nearly all of the weight.  Codes as subnormal numbers in a half's
+// lowest bits would take five instructions, but the matrix instructions sum products of subnormals with errors up to 2^-17 of
+// them.  Element e is nibble kNib[e].
 constexpr int kNib[8] = {0, 4, 1, 5, 2, 6, 3, 7};
-typedef uint32_t v4u __attribute__((ext_vector_type(4)));
-// The mask and the exponent as register values the compiler knows nothing of: with literals it takes an and and an or for
-// each pair of codes, from registers the one instruction that does both.
+// Masks and exponents as register values the compiler knows nothing of: with literals it takes an and and an or for each
+// pair of codes, from registers the one instruction that does both.
 struct Bits {
-  uint32_t mask, e6;
+  uint32_t m0, m1, e10, e6;
 };
 __device__ __forceinline__ Bits code_bits() {
-  Bits k = {0x00F000F0u, 0x54005400u};
-  asm("" : "+s"(k.mask), "+v"(k.e6));
+  Bits k = {0x000F000Fu, 0x00F000F0u, 0x64006400u, 0x54005400u};
+  asm("" : "+s"(k.m0), "+s"(k.m1), "+v"(k.e10), "+v"(k.e6));
   return k;
 }
-__device__ __forceinline__ v8h unpack(uint32_t w, const Bits& k) {
-  return __builtin_bit_cast(v8h, v4u{((w << 4) & k.mask) | k.e6, (w & k.mask) | k.e6, ((w >> 4) & k.mask) | k.e6,
-                                     ((w >> 8) & k.mask) | k.e6});
+__device__ __forceinline__ v8h unpack(uint32_t w, const Bits& k, v2h b0, v2h b1, v2h b2, v2h b3) {
+  const uint32_t w8 = w >> 8;
+  const v2h h0 = __builtin_bit_cast(v2h, (w & k.m0) | k.e10) - b0;
+  const v2h h1 = __builtin_bit_cast(v2h, (w & k.m1) | k.e6) - b1;
+  const v2h h2 = __builtin_bit_cast(v2h, (w8 & k.m0) | k.e10) - b2;
+  const v2h h3 = __builtin_bit_cast(v2h, (w8 & k.m1) | k.e6) - b3;
+  return v8h{h0[0], h0[1], h1[0], h1[1], h2[0], h2[1], h3[0], h3[1]};
 }
 
 // One of the two elements of a word of queries
@@ -150,8 +157,8 @@ struct Rows {
 struct Stage {
   uint32_t v[kStep * kD / 8];   // value codes, 64 bytes a token, 16-byte pieces of row r at piece ^ (r / 16)
   float ks[kStep], ls[kStep], rs[kStep];   // key scale log2 e / sqrt(128); log2 and reciprocal of the value scale
-  v4u kz[kStep];                // an eighth of 64 + key zero-point as fp16, eight times
-  _Float16 vz[kStep];           // 64 + value zero-point, in the order of use
+  v4h kz[kStep];                // 1024 + key zero-point twice, 64 + key zero-point twice
+  _Float16 vz[kStep];           // 1024 or 64 + value zero-point, in the order of use
 };
 constexpr int kPad = kD + 4;
 union Lds {
@@ -263,7 +270,7 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
   // offset of the lane.
   uint4 vw[4], kw[4];
   float ksl, vsl;
-  uint32_t kzl, vzl;
+  uint8_t kzl, vzl;            // (as words they are extended, and waited for, in the middle of the step before: 43.9 -> 47 us)
   Rows cur{0, false};
   int32_t ahead = 0;           // the next step's table entry
   const uint32_t koff = 64u * (uint32_t)c + 16u * (uint32_t)kg, voff = 16u * (uint32_t)lane;
@@ -288,11 +295,9 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
   }
 
   // ---- the queries: B operands, element e of step st is dimension 32 kg + 8 st + kNib[e] of row c.  A row whose largest is
-  // outside [2^-4, 2^5) is brought to [2^4, 2^5) by a power of two; what is below 2^-14 then (bf16: 2^-17) is off by 2^-25 at
-  // most.  What is to be taken off the scores, (64 + z) sum q, comes from a product of its own: -8 sum q, at most 2^15, as
-  // three fp16 parts (2^-25 off at most) in elements 0 .. 2 of lane group 0.
+  // outside [2^-4, 2^15) is brought to [2^14, 2^15) by a power of two.  A bf16 query below 2^-17 is off by 2^-25 at most then
+  // (so is the last bit of an fp16 row that is scaled down), all others are exact.
   v8h qb[RT][4];
-  v8h qz[RT];
   bool ranged = false; // whether any row has a power of two to be taken back (sh.back; all waves write the same)
   int32_t node[RT];
   {
@@ -319,35 +324,25 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
       for (int n = 0; n < 8; ++n) top = fmaxf(top, fabsf(element<BF16>(u[st][n >> 1], n & 1)));
     top = fmaxf(top, __shfl_xor(top, 16));
     top = fmaxf(top, __shfl_xor(top, 32));
-    const int ex = top > 0.f && top < INFINITY && !(top >= 0x1p-4f && top < 0x1p5f) ? 4 - ilogbf(top) : 0;
+    const int ex = top > 0.f && top < INFINITY && !(top >= 0x1p-4f && top < 0x1p15f) ? 14 - ilogbf(top) : 0;
     if (kg == 0) sh.back[16 * rt + c] = ldexpf(1.f, -ex);
     ranged |= __any(ex != 0);
-    v8h up;               // (the products' sum over all dimensions is -8 sum q in every lane of the row)
-    v4f sums = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int e = 0; e < 8; ++e) up[e] = (_Float16)-8.f;
-#pragma unroll
-    for (int st = 0; st < 4; ++st) {
+    for (int st = 0; st < 4; ++st)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const int n = kNib[e];
         qb[rt][st][e] = (_Float16)ldexpf(element<BF16>(u[st][n >> 1], n & 1), ex);
       }
-      sums = __builtin_amdgcn_mfma_f32_16x16x32_f16(up, qb[rt][st], sums, 0, 0, 0);
-    }
-    const float sum = sums[0];
-    const _Float16 z0 = (_Float16)sum, z1 = (_Float16)(sum - (float)z0), z2 = (_Float16)(sum - (float)z0 - (float)z1);
-    qz[rt] = kg == 0 ? v8h{z0, z1, z2, 0, 0, 0, 0, 0} : v8h{};
   }
   }
 
   float m[RT], l[RT];
-  v4f o[RT][8], oz[RT];        // sums of weights times 64 + code; times 64 + zero-point
+  v4f o[RT][8];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     m[rt] = kLowest;
     l[rt] = 0.f;
-    oz[rt] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) o[rt][dt] = v4f{0.f, 0.f, 0.f, 0.f};
   }
@@ -376,12 +371,11 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
       sg.ks[lane] = ksl * kScore;
       sg.ls[lane] = __builtin_amdgcn_logf(v);
       sg.rs[lane] = vsl < INFINITY ? __builtin_amdgcn_rcpf(v) : 0.f; 
-      const _Float16 zh = (_Float16)(8.f + 0.125f * (float)kzl);
-      const uint32_t z2 = __builtin_bit_cast(uint32_t, v2h{zh, zh});
-      sg.kz[lane] = v4u{z2, z2, z2, z2};
+      const _Float16 z10 = (_Float16)(1024.f + (float)kzl), z6 = (_Float16)(64.f + (float)kzl);
+      sg.kz[lane] = v4h{z10, z10, z6, z6};
       // token 16 j + 4 g + i goes to pair i of half j / 2 of lane group g, element j mod 2
       const int tj = lane >> 4, tg = (lane >> 2) & 3, ti = lane & 3;
-      sg.vz[tg * 16 + (tj >> 1) * 8 + ti * 2 + (tj & 1)] = (_Float16)(64.f + (float)vzl);
+      sg.vz[tg * 16 + (tj >> 1) * 8 + ti * 2 + (tj & 1)] = (_Float16)((ti & 1 ? 64.f : 1024.f) + (float)vzl);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         *reinterpret_cast<uint4*>(&sg.v[(16 * j + (lane >> 2)) * (kD / 8) + 4 * ((lane & 3) ^ j)]) = vw[j];
@@ -395,10 +389,12 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
 #pragma unroll
     for (int j0 = 0; j0 < 4; j0 += TJ) {
       v4f acc[TJ][RT];
-      v8h z[TJ];
+      v2h b10[TJ], b6[TJ];
 #pragma unroll
       for (int j = 0; j < TJ; ++j) {
-        z[j] = __builtin_bit_cast(v8h, sg.kz[16 * (j0 + j) + c]);
+        const v4h z = sg.kz[16 * (j0 + j) + c];
+        b10[j] = v2h{z[0], z[1]};
+        b6[j] = v2h{z[2], z[3]};
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) acc[j][rt] = v4f{0.f, 0.f, 0.f, 0.f};
       }
@@ -407,14 +403,10 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
 #pragma unroll
         for (int j = 0; j < TJ; ++j) {
           const uint4& u = kw[j0 + j];
-          const v8h kd = unpack(st == 0 ? u.x : st == 1 ? u.y : st == 2 ? u.z : u.w, bits);
+          const v8h kd = unpack(st == 0 ? u.x : st == 1 ? u.y : st == 2 ? u.z : u.w, bits, b10[j], b6[j], b10[j], b6[j]);
 #pragma unroll
           for (int rt = 0; rt < RT; ++rt) acc[j][rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kd, qb[rt][st], acc[j][rt], 0, 0, 0);
         }
-#pragma unroll
-      for (int j = 0; j < TJ; ++j)
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) acc[j][rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(z[j], qz[rt], acc[j][rt], 0, 0, 0);
 #pragma unroll
       for (int j = 0; j < TJ; ++j) {
         const v4f k4 = *reinterpret_cast<const v4f*>(&sg.ks[16 * (j0 + j) + 4 * kg]);
@@ -482,7 +474,6 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
         const float mn = fmaxf(m[rt], top - kTop), f = __builtin_amdgcn_exp2f(m[rt] - mn);
         l[rt] = scaled(l[rt], m[rt] - mn);
         m[rt] = mn;
-        oz[rt] *= f;
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt) o[rt][dt] *= f;
       }
@@ -527,14 +518,14 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-    // ---- values: A = 16 dimensions x 32 tokens of 64 + code.  The transposing read hands lane (c, kg) the 16 codes of
-    // dimension 16 dt + c whose rows the 16 lanes of its group name: token 16 (c / 4) + 4 kg + c mod 4, nibble c.  The
-    // zero-points are one more tile, the same for all 16 of its dimensions.
+    // ---- values: A = 16 dimensions x 32 tokens of code - z.  The transposing read hands lane (c, kg) the 16 codes of
+    // dimension 16 dt + c whose rows the 16 lanes of its group name: token 16 (c / 4) + 4 kg + c mod 4, nibble c.
     {
+      v8h bz[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) bz[h] = *reinterpret_cast<const v8h*>(&sg.vz[16 * kg + 8 * h]);
       const int row = 16 * (c >> 2) + 4 * kg + (c & 3);
-      // Dimension tiles at a time, for four independent sums; the next ones' reads go ahead of them, as the scores' products
-      // go ahead of that with the zero-points, whose operands come from LDS (both, RT = 1: chains of 5 for 16 sequences
-      // 38.4 -> 37.0 us, 32 ragged sequences of one token 44.5 -> 42.7).
+      // Dimension tiles at a time, for four independent sums; the next ones' reads go ahead of them.
       constexpr int TD = 4 / RT;
       v2i t[2][TD];
       auto read = [&](int d0, v2i (&t)[TD]) {
@@ -546,14 +537,6 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
       };
       read(0, t[0]);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const v8h z = *reinterpret_cast<const v8h*>(&sg.vz[16 * kg + 8 * h]);
-#pragma unroll
-        for (int part = 0; part < 2; ++part)
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt) oz[rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(z, part ? alo[rt][h] : ahi[rt][h], oz[rt], 0, 0, 0);
-      }
-#pragma unroll
       for (int d0 = 0; d0 < 8; d0 += TD) {
         if (d0 + TD < 8) read(d0 + TD, t[(d0 / TD + 1) & 1]);
         __builtin_amdgcn_sched_barrier(0);
@@ -563,7 +546,8 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
 #pragma unroll
           for (int d = 0; d < TD; ++d) {
             const v2i x = t[(d0 / TD) & 1][d];
-            va[d] = unpack(h ? (uint32_t)x.y : (uint32_t)x.x, bits);
+            va[d] = unpack(h ? (uint32_t)x.y : (uint32_t)x.x, bits, v2h{bz[h][0], bz[h][1]}, v2h{bz[h][2], bz[h][3]},
+                           v2h{bz[h][4], bz[h][5]}, v2h{bz[h][6], bz[h][7]});
           }
 #pragma unroll
           for (int part = 0; part < 2; ++part)
@@ -606,7 +590,7 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
     for (int w = 1; w < kWaves; ++w) M = fmaxf(M, stat[0][w][16 * rt + c2]);
     const float f = __builtin_amdgcn_exp2f(m[rt] - M);
 #pragma unroll
-    for (int dt = 0; dt < 8; ++dt) *reinterpret_cast<v4f*>(&lds.sum[wave][c2][16 * dt + 4 * kg2]) = (o[rt][dt] - oz[rt]) * f;
+    for (int dt = 0; dt < 8; ++dt) *reinterpret_cast<v4f*>(&lds.sum[wave][c2][16 * dt + 4 * kg2]) = o[rt][dt] * f;
     __syncthreads();
     const int row = tid >> 4, d0 = (tid & 15) * 8, r = r0 + 16 * rt + row;
     float Mr = stat[0][0][16 * rt + row], L = 0.f;

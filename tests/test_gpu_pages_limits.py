@@ -83,3 +83,45 @@ def test_scores_at_the_ends_of_fp32(Q):  # noqa: F811
             assert torch.isfinite(c.q.float()).all()
             y = c.run(Q).float().cpu()
             assert (y - ref).abs().le(ref.abs() * (2.0 ** -8 + 2.0 ** -20)).all(), (kscale, sign)
+
+
+def test_long_sums_keep_their_smallest_parts(Q):  # noqa: F811
+    """65536 tokens of one unit in one workgroup (513 sequences, the others empty).  The first 256 have nearly all of the
+    weight and the value 0 in half of the dimensions (code = zero-point = 7); what the others add there, code 15, is each
+    time about half a step of 64 + code times the weights' sum, and must not be lost or rounded up."""
+    T, P, B = 65536, 64, 513
+    pages = T // P
+    cache = Q.KV4Pages.empty(pages, P, 1)
+    k, v = np.full((pages, 1, P, 64), 0x77, np.uint8), np.full((pages, 1, P, 64), 0xFF, np.uint8)
+    head = 256 // P
+    k[:head, ..., 0] = 0x7F                     # dimension 0: code 15, 8 steps over the zero-point
+    k[head:, ..., 0] = 0x77
+    v[:head, ..., :32] = 0x77                   # dimensions 0 .. 63: code 7, value 0
+    v[head:, ..., 32:] = 0x00                   # dimensions 64 .. 127 of the tail: code 0
+    for side, codes in ((cache.k, k), (cache.v, v)):
+        side.codes.copy_(tensor(codes))
+        side.scales.fill_(1.0)
+        side.zeros.fill_(7)
+    table = torch.zeros((B, pages), dtype=torch.int32, device="cuda")
+    table[0] = torch.arange(pages, dtype=torch.int32, device="cuda")
+    starts = torch.ones(B + 1, dtype=torch.int32, device="cuda")
+    starts[0] = 0
+    lens = torch.zeros(B, dtype=torch.int32, device="cuda")
+    lens[0] = T
+    # heads of different weight of the tail: 32 79 w is (i + 0.55) steps of the sum 71 * 64 of a wave
+    w = (np.arange(16) * 0.37 + 0.55) * 2.0 ** -11 / (32 * 79)
+    q = np.zeros((1, 16, 128))
+    q[0, :, 0] = -np.log(w) * np.sqrt(128.0) / 8
+    q = torch.from_numpy(q).half()
+    y = values(Q.kv4_attention_tree(q.cuda(), cache, table, starts, lens, max_nodes=1, max_len=T)).astype(np.float64)
+    assert Q.device_error() == 0
+    score = q[0, :, 0].double().numpy() * 8 / np.sqrt(128.0)
+    p = np.exp(-score)
+    total = 256 + (T - 256) * p
+    ref = np.concatenate([np.repeat((8 * (T - 256) * p / total)[:, None], 64, axis=1),
+                          np.repeat(((8 * 256 - 7 * (T - 256) * p) / total)[:, None], 64, axis=1)], axis=1)
+    # test_gpu_pages' limit: S = score, L = 0, the largest value 8
+    limit = HALF[torch.float16] * np.abs(ref) + (2 * (score[:, None] + 1) * 2.0 ** -21 + 2.0 ** -21 + T / 32 * 2.0 ** -24) * 8 + 2.0 ** -25
+    over = np.abs(y[0] - ref) / limit
+    print("worst error", over[:, :64].max(), over[:, 64:].max(), "of the limit", flush=True)
+    assert over.max() <= 1.0
