@@ -124,13 +124,12 @@ size_t qift_kv4_attention_tree_workspace_bytes(int64_t B, int32_t Hq, int32_t Hk
  * [2^-4, 2^15) is scaled by a power of two that brings it to [2^14, 2^15); a bf16 row's queries that are
  * below 2^-17 then, and those of an fp16 row that is scaled down below 2^-14, are off by 2^-25 at most, all
  * others exact.  The result is within half a step of its type and
- *   (2 (S + L) + 14 + lens[b] / 100) 2^-21
+ *   (2 (S + L) + 14 + lens[b] / 256) 2^-21
  * of the KV head's largest value, S the largest |q| |k_hat| / sqrt(128) of the row and L the largest |log2|
  * of a value scale that it sees: with u = 2^-24, a score takes 7 u S (four sums of products, the key's scale,
  * the conversion to a power of two, the value's scale), a weight 2 u L more, both count in the numerator and
  * in the denominator; a wave's sum of values has lens[b] / 64 instructions' roundings, its sum of weights
- * lens[b] / 16; the rest are the exponentials, the joining of waves and parts and the
- * division.
+ * lens[b] / 256; the rest are the exponentials, the joining of waves and parts and the division.
  * Value scales under 2^-90 count as 2^-90.  A score that with log2 of its value's scale, both as powers of
  * two, is past fp32's lowest value counts as not seen; past its largest, the row is NaN.
  * B = 0 or rows = 0 does nothing.  Limits: 1 <= max_nodes <= 256, Hq a multiple of Hkv and

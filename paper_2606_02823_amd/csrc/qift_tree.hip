@@ -496,6 +496,9 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
         }
       }
     }
+    float add[RT];               // the step's sum of exponentials: the running one then rounds once a step, not 16 times
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) add[rt] = 0.f;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       // half h, pair i: tokens 16 (2 h) + 4 kg + i and 16 (2 h + 1) + 4 kg + i
@@ -506,8 +509,8 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float x = __builtin_amdgcn_exp2f(y[rt][2 * h][i] - m[rt]), z = __builtin_amdgcn_exp2f(y[rt][2 * h + 1][i] - m[rt]);
-          l[rt] = fmaf(x, r0[i], l[rt]);
-          l[rt] = fmaf(z, r1[i], l[rt]);
+          add[rt] = fmaf(x, r0[i], add[rt]);
+          add[rt] = fmaf(z, r1[i], add[rt]);
           const v2h hi = __builtin_bit_cast(v2h, __builtin_amdgcn_cvt_pkrtz(x, z));
           const v2h lo = __builtin_bit_cast(v2h, __builtin_amdgcn_cvt_pkrtz(less_low(x, hi), less_high(z, hi)));
           ahi[rt][h][2 * i] = hi[0];
@@ -518,6 +521,8 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
       }
       __builtin_amdgcn_sched_barrier(0);
     }
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) l[rt] += add[rt];
     // ---- values: A = 16 dimensions x 32 tokens of code - z.  The transposing read hands lane (c, kg) the 16 codes of
     // dimension 16 dt + c whose rows the 16 lanes of its group name: token 16 (c / 4) + 4 kg + c mod 4, nibble c.
     {

@@ -125,3 +125,38 @@ def test_long_sums_keep_their_smallest_parts(Q):  # noqa: F811
     over = np.abs(y[0] - ref) / limit
     print("worst error", over[:, :64].max(), over[:, 64:].max(), "of the limit", flush=True)
     assert over.max() <= 1.0
+
+
+def test_long_sums_of_weights(Q):  # noqa: F811
+    """2^20 tokens of one unit in one workgroup: the first 256 have the value 8 and nearly all of the weight, each of the
+    others half a step, a little more or less, of what a lane has summed by then (16 tokens of weight 1: 2^-19 a step).  Added one
+    by one they would all be lost or all count for a whole step."""
+    T, P, B = 1 << 20, 64, 513
+    pages = T // P
+    cache = Q.KV4Pages.empty(pages, P, 1)
+    for side in (cache.k, cache.v):
+        side.codes.fill_(0x77)                  # code = zero-point
+        side.scales.fill_(1.0)
+        side.zeros.fill_(7)
+    cache.k.codes[:256 // P, ..., 0] = 0x7F     # dimension 0: code 15, 8 steps over the zero-point
+    cache.v.codes[:256 // P] = 0xFF
+    table = torch.zeros((B, pages), dtype=torch.int32, device="cuda")
+    table[0] = torch.arange(pages, dtype=torch.int32, device="cuda")
+    starts = torch.ones(B + 1, dtype=torch.int32, device="cuda")
+    starts[0] = 0
+    lens = torch.zeros(B, dtype=torch.int32, device="cuda")
+    lens[0] = T
+    w = np.repeat([0.45, 0.48, 0.52, 0.55], 4) * 2.0 ** -19
+    q = np.zeros((1, 16, 128))
+    q[0, :, 0] = -np.log(w) * np.sqrt(128.0) / 8
+    q = torch.from_numpy(q).half()
+    y = values(Q.kv4_attention_tree(q.cuda(), cache, table, starts, lens, max_nodes=1, max_len=T)).astype(np.float64)
+    assert Q.device_error() == 0
+    score = q[0, :, 0].double().numpy() * 8 / np.sqrt(128.0)
+    ref = (8 * 256 / (256 + (T - 256) * np.exp(-score)))[:, None]
+    # half a step, and the sums: 16 roundings within a step of 64 tokens, then one for each of T / 256 steps of a wave; a value
+    # sum's T / 64; scores 7 2^-24 S in numerator and denominator; 2^-18 for all that does not grow
+    limit = HALF[torch.float16] * ref + (2 * 7 * score[:, None] * 2.0 ** -24 + 2.0 ** -18 + (T / 64 + T / 256) * 2.0 ** -24) * 8
+    over = np.abs(y[0] - ref) / limit
+    print("worst error", over.max(), "of the limit", flush=True)
+    assert over.max() <= 1.0
