@@ -81,9 +81,10 @@ int qift_kv4_append(const qift_kv4_pages *cache, const void *k, const void *v, i
 int qift_kv4_read(const qift_kv4_pages *cache, const int32_t *slots, int64_t n, int32_t dtype,
                   void *k_values, void *v_values, qift_stream_t stream);
 
-/* Workspace bytes of qift_kv4_attention_tree for these limits; 0 for an unsupported shape, and where the
- * call needs none.  It grows with max_nodes and max_len, but not evenly: ask for the limits that the
- * call is made with. */
+/* Workspace bytes that are enough for every call of qift_kv4_attention_tree with these heads whose B, max_nodes
+ * and max_len are at most these: it grows with each of them, and stays below 26 MB.  0 where no such call
+ * needs any, and for an unsupported shape.  (A call asks for what its own limits need, which may be less: one
+ * that has work for every CU without cutting sequences needs none.) */
 size_t qift_kv4_attention_tree_workspace_bytes(int64_t B, int32_t Hq, int32_t Hkv, int32_t head_dim,
                                                int32_t max_nodes, int64_t max_len);
 

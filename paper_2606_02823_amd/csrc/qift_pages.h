@@ -106,6 +106,7 @@ struct Plan {
   int32_t shares;       // workgroups of a block of rows; 0: one to a unit
 };
 QIFT_HD int32_t rounds_of(int32_t len) { return len < 1 ? 1 : (int32_t)(((int64_t)len + kRound - 1) / kRound); }
+inline int64_t dealt_below(int64_t max_len) { return max_len <= kFewRounds * kRound ? 256 : 1024; }   // units times blocks
 inline Plan plan(int64_t B, int32_t Hkv, int32_t G, int32_t max_nodes, int64_t max_len) {
   Plan p;
   const int64_t rows = (int64_t)max_nodes * G;
@@ -113,7 +114,7 @@ inline Plan plan(int64_t B, int32_t Hkv, int32_t G, int32_t max_nodes, int64_t m
   p.blocks = (int32_t)((rows + 16 * p.rt - 1) / (16 * p.rt));
   const int64_t units = B * Hkv, rounds = (max_len + kRound - 1) / kRound;
   p.shares = 0;
-  if (rounds > 1 && B <= kMostShared && units * p.blocks < (rounds <= kFewRounds ? 256 : 1024)) {
+  if (rounds > 1 && B <= kMostShared && units * p.blocks < dealt_below(max_len)) {
     int64_t n = 512 / p.blocks;                 // two workgroups to each of 256 CUs
     if (n > units * (rounds + kBegin)) n = units * (rounds + kBegin);
     p.shares = n < 1 ? 1 : (int32_t)n;
@@ -143,6 +144,26 @@ QIFT_HD int32_t round_at(int32_t slot) { return slot > kBegin ? slot - kBegin : 
 inline int64_t records(const Plan& p, int64_t B, int32_t Hkv) { return p.shares == 0 ? 0 : p.shares + B * Hkv; }
 inline int64_t workspace_words(const Plan& p, int64_t B, int32_t Hkv, int32_t G, int32_t max_nodes) {
   return p.shares == 0 ? 0 : records(p, B, Hkv) * ((int64_t)max_nodes * G) * 130 + 2 * B * Hkv;
+}
+
+// Words that are enough for every call with at most B sequences, max_nodes nodes and max_len tokens.  A call with fewer nodes
+// may be dealt out where one with more is not, and has more shares of a block where it has fewer blocks, so each number of
+// blocks is asked with the most nodes that it has and the most sequences that are dealt out then; a longer max_len only adds.
+inline int64_t most_workspace_words(int64_t B, int32_t Hkv, int32_t G, int32_t max_nodes, int64_t max_len) {
+  int64_t most = 0;
+  for (int32_t nodes = max_nodes; nodes > 0;) {
+    const Plan one = plan(1, Hkv, G, nodes, max_len);
+    const int64_t per = (int64_t)Hkv * one.blocks;
+    int64_t b = (dealt_below(max_len) - 1) / per;
+    if (b > kMostShared) b = kMostShared;
+    if (b > B) b = B;
+    if (b > 0) {
+      const int64_t w = workspace_words(plan(b, Hkv, G, nodes, max_len), b, Hkv, G, nodes);
+      if (w > most) most = w;
+    }
+    nodes = one.rt == 1 ? 0 : one.blocks == 1 ? 16 / G : (one.blocks - 1) * 32 / G;
+  }
+  return most;
 }
 
 }  // namespace pages

@@ -82,8 +82,7 @@ int qift_kv4_read(const qift_kv4_pages* cache, const int32_t* slots, int64_t n, 
 size_t qift_kv4_attention_tree_workspace_bytes(int64_t B, int32_t Hq, int32_t Hkv, int32_t head_dim, int32_t max_nodes,
                                                int64_t max_len) {
   if (!tree_shape_ok(B, Hq, Hkv, head_dim, max_nodes, max_len) || B == 0) return 0;
-  const qift::pages::Plan p = qift::pages::plan(B, Hkv, Hq / Hkv, max_nodes, max_len);
-  return (size_t)qift::pages::workspace_words(p, B, Hkv, Hq / Hkv, max_nodes) * sizeof(float);
+  return (size_t)qift::pages::most_workspace_words(B, Hkv, Hq / Hkv, max_nodes, max_len) * sizeof(float);
 }
 
 int qift_kv4_attention_tree(const qift_kv4_pages* cache, const void* q, int64_t q_stride, int32_t dtype, int64_t rows,
@@ -99,7 +98,9 @@ int qift_kv4_attention_tree(const qift_kv4_pages* cache, const void* q, int64_t 
   if (!q || !table || !starts || !lens || !out) return QIFT_ERR_NULL;
   st = check_pointers(cache);
   if (st != QIFT_OK) return st;
-  const size_t need = qift_kv4_attention_tree_workspace_bytes(B, Hq, cache->Hkv, cache->head_dim, max_nodes, max_len);
+  const int32_t Hkv = cache->Hkv, G = Hq / Hkv;
+  const size_t need =
+      (size_t)qift::pages::workspace_words(qift::pages::plan(B, Hkv, G, max_nodes, max_len), B, Hkv, G, max_nodes) * sizeof(float);
   if (need > 0 && (!workspace || workspace_bytes < need)) return QIFT_ERR_WORKSPACE;
   if (!aligned(q, 16) || q_stride % 8 || !aligned(out, 16) || !aligned(table, 4) || !aligned(starts, 4) ||
       !aligned(lens, 4) || (visible && !aligned(visible, 8)) || (need > 0 && !aligned(workspace, 16)))

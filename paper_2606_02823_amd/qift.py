@@ -554,7 +554,7 @@ def kv4_read(cache: KV4Pages, slots: torch.Tensor, dtype=torch.float16, out=None
 
 
 def kv4_attention_tree_workspace(B: int, Hq: int, Hkv: int, max_nodes: int, max_len: int, device="cuda") -> torch.Tensor:
-    """A workspace for kv4_attention_tree calls with these limits (one call at a time)."""
+    """A workspace for kv4_attention_tree calls with at most these sequences, nodes and lengths (one call at a time)."""
     need = int(lib().qift_kv4_attention_tree_workspace_bytes(B, Hq, Hkv, 128, max_nodes, max_len))
     return torch.empty(max(need, 16), dtype=torch.uint8, device=device)
 

@@ -429,3 +429,31 @@ def test_nodes_that_are_left_out_do_not_move_the_others(ask):
         assert row0 == s0 and n == min(nodes, rows - s0, most_nodes)
         assert ctx == max(0, ln - nodes)
         assert length == (ln if n == nodes else min(ln, ctx + n))
+
+
+def test_workspace_covers_every_smaller_call(L):
+    """A workspace of the queried size serves every call whose sequences, nodes and lengths are at most the queried ones, and
+    the query grows with each of them; a call itself asks for what its own plan needs, which may be less."""
+    ws = L.qift_kv4_attention_tree_workspace_bytes
+
+    def enough(B, Hq, Hkv, nodes, length, size):   # (misaligned queries are refused after the size, and nothing is launched)
+        st = L.qift_kv4_attention_tree(pool(Hkv=Hkv), MIS, Hq * 128, 0, 5, A, 100, A, A, B, Hq, nodes, length, None, A, A, size, None)
+        assert st in (E_ALIGN, E_WS)
+        return st == E_ALIGN
+    # the server of 16 sequences whose largest step is 64 nodes over 8192 tokens
+    most = ws(16, 32, 8, 128, 64, 8192)
+    assert most > 0
+    for nodes in range(1, 65):
+        assert enough(16, 32, 8, nodes, 8192, most), nodes
+    rng = np.random.default_rng(14)
+    for _ in range(300):
+        Hkv, G = int(rng.choice([1, 2, 4, 8, 32])), int(rng.choice([1, 2, 3, 4, 8, 64]))
+        B, nodes, length = int(np.exp(rng.uniform(0, 7))), int(rng.integers(1, 257)), int(np.exp(rng.uniform(0, 12)))
+        size = ws(B, Hkv * G, Hkv, 128, nodes, length)
+        assert size < 26e6
+        for _ in range(12):
+            b, n, t = int(rng.integers(1, B + 1)), int(rng.integers(1, nodes + 1)), int(rng.integers(1, length + 1))
+            assert enough(b, Hkv * G, Hkv, n, t, size), (B, Hkv, G, nodes, length, b, n, t)
+            assert ws(b, Hkv * G, Hkv, 128, n, t) <= size
+    # no call of one round of tokens needs any
+    assert ws(600, 32, 8, 128, 256, 256) == 0 and enough(600, 32, 8, 256, 256, 0)
