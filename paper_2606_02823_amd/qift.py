@@ -502,6 +502,8 @@ def _rows(t, index, dtype, shape, name) -> int:
 
 def _run(index, call, args, stream):
     """The call on its device (kernels are launched on the current device and its current stream)."""
+    if stream is not None and getattr(stream, "device_index", index) != index:
+        raise ValueError(f"the stream is on device {stream.device_index}, the cache on device {index}")
     if (_raw_device() if _raw_device is not None else torch.cuda.current_device()) == index:
         return call(*args, _stream(stream))
     with torch.cuda.device(index):

@@ -457,3 +457,13 @@ def test_workspace_covers_every_smaller_call(L):
             assert ws(b, Hkv * G, Hkv, 128, n, t) <= size
     # no call of one round of tokens needs any
     assert ws(600, 32, 8, 128, 256, 256) == 0 and enough(600, 32, 8, 256, 256, 0)
+
+
+def test_binding_refuses_a_stream_of_another_device():
+    """Kernels are launched on the cache's device: a stream of another one would run them there, on memory it may not reach."""
+    from types import SimpleNamespace
+
+    def call(*args):
+        raise AssertionError("the call must not be reached")
+    with pytest.raises(ValueError, match="stream"):
+        qift._run(0, call, (), SimpleNamespace(device_index=1, cuda_stream=0))
