@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from oracle import pages as opages
-from test_gpu_pages import HALF, Case, Q, random_tree, tensor, values   # noqa: F401
+from test_gpu_pages import HALF, Case, Q, cache_of, draw_groups, host, random_tree, same_cache, tensor, values   # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -160,3 +160,85 @@ def test_long_sums_of_weights(Q):  # noqa: F811
     over = np.abs(y[0] - ref) / limit
     print("worst error", over.max(), "of the limit", flush=True)
     assert over.max() <= 1.0
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16], ids=["fp16", "bf16"])
+def test_many_tokens_against_the_oracle(Q, dtype):  # noqa: F811
+    """Enough rows for the reading kernel of four tiles a workgroup, the last of them not full; slots in any order, some of
+    none; the outputs given by the caller."""
+    rng = np.random.default_rng(21)
+    n, Hkv, page = 4133, 8, 48
+    pages = -(-n // page) + 2
+    cache = cache_of(Q, rng, pages, page, Hkv)
+    before = host(cache.k), host(cache.v)
+    slots = rng.permutation(pages * page)[:n].astype(np.int32)
+    slots[[5, 700, n - 1]] = -1
+    k, v = (draw_groups(rng, n, Hkv, dtype) for _ in range(2))
+    given = [torch.full((n, Hkv, 128), float("nan"), dtype=dtype, device="cuda") for _ in range(2)]
+    got = Q.kv4_append(cache, k.cuda(), v.cuda(), tensor(slots), values=(given[0], given[1]))
+    assert got[0] is given[0] and got[1] is given[1]
+    for side, was, x, y in ((cache.k, before[0], k, got[0]), (cache.v, before[1], v, got[1])):
+        *want, hat = opages.append(*was, values(x), slots)
+        same_cache(side, want)
+        assert torch.equal(y.cpu(), torch.from_numpy(hat).to(dtype))
+    for out in (torch.float16, torch.bfloat16, torch.float32):
+        given = [torch.full((n, Hkv, 128), float("nan"), dtype=out, device="cuda") for _ in range(2)]
+        back = Q.kv4_read(cache, tensor(slots), dtype=out, out=given)
+        assert back[0] is given[0] and back[1] is given[1]
+        for side, y in ((cache.k, back[0]), (cache.v, back[1])):
+            assert torch.equal(y.cpu(), torch.from_numpy(opages.read(*host(side), slots)).to(out))
+    assert Q.device_error() == 0
+
+
+def test_given_outputs_are_checked(Q):  # noqa: F811
+    cache = Q.KV4Pages.empty(2, 16, 4)
+    x = torch.zeros((3, 4, 128), dtype=torch.float16, device="cuda")
+    slots = torch.arange(3, dtype=torch.int32, device="cuda")
+    good = torch.empty_like(x)
+    for bad, err in ((good.float(), TypeError), (good[:2], ValueError), (good.cpu(), TypeError), (good.bfloat16(), TypeError),
+                     (torch.empty((3, 8, 128), dtype=torch.float16, device="cuda")[:, ::2], ValueError)):
+        for pair in ((bad, good), (good, bad)):
+            with pytest.raises(err):
+                Q.kv4_append(cache, x, x, slots, values=pair)
+            with pytest.raises(err):
+                Q.kv4_read(cache, slots, out=pair)
+    assert not cache.k.scales.any() and Q.device_error() == 0
+
+
+def test_calls_with_everything_given_allocate_nothing(Q):  # noqa: F811
+    c = Case(Q, 122, [(3, 900), (5, 2000)], 16, 4, 32, torch.float16)
+    args = [c.q.cuda(), c.cache, tensor(c.table), tensor(c.starts), tensor(c.lens)]
+    out = torch.empty_like(args[0])
+    ws = Q.kv4_attention_tree_workspace(2, 16, 4, 5, 2000)
+    k = torch.randn((8, 4, 128), device="cuda").half()
+    pair = torch.empty_like(k), torch.empty_like(k)
+    slots = tensor(c.slots(0, np.arange(8)))
+
+    def calls():
+        Q.kv4_append(c.cache, k, k, slots, values=pair)
+        Q.kv4_read(c.cache, slots, out=pair)
+        Q.kv4_attention_tree(*args, max_nodes=5, max_len=2000, out=out, workspace=ws)
+    calls()
+    torch.cuda.synchronize()
+    was = torch.cuda.memory_stats()["allocation.all.allocated"], torch.cuda.mem_get_info()[0]
+    for _ in range(3):
+        calls()
+    torch.cuda.synchronize()
+    assert (torch.cuda.memory_stats()["allocation.all.allocated"], torch.cuda.mem_get_info()[0]) == was
+
+
+def test_steps_of_a_server(Q):  # noqa: F811
+    """A chunk of a prompt beside sequences of one token, dealt out and whole; 130 sequences of one token, one of them long; a long
+    sequence whose values the whole length weighs."""
+    rng = np.random.default_rng(22)
+    seqs = [(1, int(t)) for t in rng.integers(1, 900, 15)] + [(256, 700)] + [(1, int(t)) for t in rng.integers(1, 900, 15)]
+    c = Case(Q, 123, seqs, 8, 2, 32, torch.bfloat16)
+    c.check(c.run(Q), "chunk and tokens")
+    c = Case(Q, 126, seqs[12:19], 8, 2, 32, torch.bfloat16)
+    c.check(c.run(Q, max_len=2000), "chunk and tokens, dealt out")
+    seqs = [(1, int(t)) for t in rng.integers(1, 60, 129)] + [(1, 9000)]
+    c = Case(Q, 124, seqs, 32, 8, 16, torch.float16)
+    c.check(c.run(Q), "130 users")
+    c = Case(Q, 125, [(2, 40000)], 8, 2, 128, torch.float16, gain=0.2)
+    c.check(c.run(Q), "40000 tokens")
+    assert Q.device_error() == 0

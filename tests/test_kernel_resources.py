@@ -54,3 +54,13 @@ def test_scale_search_leaves_four_workgroups_a_cu():
     assert len(search) == 20
     for k, v in search.items():
         assert v[".group_segment_fixed_size"] <= 40960 and v[".vgpr_count"] <= 128, k
+
+
+@pytest.mark.parametrize("name", ["k_tree", "k_tree_merge", "k_append", "k_read"])
+def test_no_spills_in_the_paged_kernels(name):
+    ks = {k: v for k, v in kernels(qift.LIB_PATH).items() if f"{len(name)}{name}" in k}
+    assert len(ks) == {"k_tree": 4, "k_tree_merge": 1, "k_append": 2, "k_read": 6}[name]
+    assert not {k: v[".vgpr_spill_count"] for k, v in ks.items() if v[".vgpr_spill_count"] or v[".private_segment_fixed_size"]}
+    # two workgroups of the attention to a CU: 256 registers a lane, half of the 160 KB each
+    if name == "k_tree":
+        assert all(v[".vgpr_count"] <= 256 and v[".group_segment_fixed_size"] <= 81920 for v in ks.values())

@@ -467,3 +467,10 @@ def test_binding_refuses_a_stream_of_another_device():
         raise AssertionError("the call must not be reached")
     with pytest.raises(ValueError, match="stream"):
         qift._run(0, call, (), SimpleNamespace(device_index=1, cuda_stream=0))
+
+
+def test_plan_has_row_tiles_that_the_kernel_is_built_for(ask):
+    lines = [("plan", B, Hkv, G, nodes, length) for B in (1, 7, 600) for Hkv in (1, 8) for G in (1, 3, 4, 64) for nodes in (1, 4, 5, 16, 17, 256)
+             for length in (1, 257, 5000)]
+    for (_, _, _, G, nodes, _), (rt, blocks, *_) in zip(lines, ask(lines)):
+        assert rt == (1 if nodes * G <= 16 else 2) and blocks == -(-nodes * G // (16 * rt))
