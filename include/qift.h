@@ -579,6 +579,7 @@ int qift_last_hip_error(void);
  * so every kernel exits; the results of the affected call are then not to be
  * trusted.  Bits: QIFT_DEVERR_GROUP_WAIT (a wave barrier inside a
  * workgroup), QIFT_DEVERR_CHAIN_WAIT (a wait for another workgroup).
+ * (The paged cache's calls add QIFT_DEVERR_INDEX for device data outside its range: qift_pages.h.)
  * qift_device_error synchronizes the stream, writes the word of the current
  * device to *bits (host) and, if clear is non-zero, resets it.  Not
  * capturable in a HIP graph.

@@ -115,6 +115,10 @@ size_t qift_kv4_attention_tree_workspace_bytes(int64_t B, int32_t Hq, int32_t Hk
  *              the nodes past lens[b] have no position and are not seen.
  *   max_nodes, max_len   host: what n_b and lens[b] may reach in this call (they size the launch and
  *              the workspace, so a captured call serves any content up to them).
+ *              They also decide how work is cut: from 1024 on of B * Hkv * ceil(max_nodes * Hq / Hkv / 32)
+ *              (256 where max_len <= 1024), and for B > 512, each (sequence, KV head, 32 rows) is one
+ *              workgroup's whatever its length, so a batch of very different lengths or node counts is
+ *              faster in two calls then.
  *   visible    uint64 [rows][ceil(max_nodes / 64)], 8-byte aligned, nullable.
  *   out        out: [rows][Hq][128] in q's type.
  *   workspace  device scratch of qift_kv4_attention_tree_workspace_bytes bytes (16-byte aligned;

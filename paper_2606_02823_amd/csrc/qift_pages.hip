@@ -33,8 +33,8 @@ struct Side {
 
 // Workgroup (tile, side, head), heads fastest, of 16 tokens, its group of lanes l / 16 the token 16 tile + l / 16.  Bound by
 // its bytes (without its arithmetic it takes as long), and those come best when the heads of a token are read together:
-// 16384 tokens of 8 heads with the values written, 152 MB, 37.4 us with the tiles fastest, 32.0 so (4.7 TB/s; 30.7 us at a
-// large copy's rate).  More tiles to a workgroup, their loads ahead, were no faster.
+// 16384 tokens of 8 heads with the values written, 152 MB, 36.7 us with the tiles fastest, 32.1 so (4.7 TB/s; 31.0 us at a
+// large copy's rate; all times here are of captured calls on two caches in turn, so that the Infinity Cache holds neither).  More tiles to a workgroup, their loads ahead, were no faster.
 template <bool BF16>
 __global__ __launch_bounds__(256) void k_append(const uint16_t* __restrict__ k, const uint16_t* __restrict__ v,
                                                 int64_t ks, int64_t vs, const int32_t* __restrict__ slots, int n,
@@ -69,8 +69,8 @@ __global__ __launch_bounds__(256) void k_append(const uint16_t* __restrict__ k, 
 }
 
 // N tiles of 16 tokens of a head and side to a workgroup, every load sent before the first is used.  Bound by its bytes, most
-// of them written: 32768 tokens of 8 heads to bf16, 170 MB, 37 us (4.6 TB/s; 34 us at a large copy's rate); here the
-// tiles are fastest (heads fastest: 40 us).
+// of them written: 32768 tokens of 8 heads to bf16, 170 MB, 36.6 us (4.7 TB/s; 34.7 us at a large copy's rate);
+// here the tiles are fastest (heads fastest: 40 us).
 template <int DT, int N>
 __global__ __launch_bounds__(256) void k_read(const int32_t* __restrict__ slots, int n, pages::Div page, uint32_t Hkv,
                                               uint32_t capacity, Side kc, Side vc, void* __restrict__ ko,
@@ -131,8 +131,8 @@ hipError_t launch_kv4_append(const Kv4Pool& c, const uint16_t* k, const uint16_t
 
 hipError_t launch_kv4_read(const Kv4Pool& c, const int32_t* slots, int64_t n, int dtype, void* ko, void* vo,
                            hipStream_t s) {
-  // four tiles to a workgroup where that leaves at least four workgroups to a CU: 32768 tokens of 8 heads 46 -> 37 us,
-  // 333 of 32 heads 4.0 against 4.7
+  // four tiles to a workgroup where that leaves at least four workgroups to a CU: 32768 tokens of 8 heads 46.4 -> 36.6 us,
+  // 333 of 32 heads 4.1 against 4.5
   const bool wide = n * c.Hkv * 2 >= 65536;
   const dim3 grid((unsigned)((n + (wide ? 63 : 15)) / (wide ? 64 : 16)), (unsigned)c.Hkv, 2);
   const pages::Div page = pages::make_div((uint32_t)c.page);

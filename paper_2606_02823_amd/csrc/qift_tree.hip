@@ -98,9 +98,9 @@ __device__ __forceinline__ int thread_again() {
 // every byte), is subtracted.  Left in the operands, with its share taken from the sums by one more product, the base would
 // save two of these nine instructions a word (16 trees of 64 nodes 264 us, then 255; chains of 5 for 16 sequences 37.3, 35.9;
 // 32 ragged sequences 43.9, 42.0), but the sums would be of 64 to 79 times the weights and round as such: up to 2^-9 of the
-// largest value was lost so over 65536 tokens whose first have nearly all of the weight.  Codes as subnormal numbers in a half's
-// lowest bits would take five instructions, but the matrix instructions sum products of subnormals with errors up to 2^-17 of
-// them.  Element e is nibble kNib[e].
+// largest value was lost so over 65536 tokens whose first have nearly all of the weight.  Codes as subnormal numbers in a
+// half's lowest bits would take five instructions, but the matrix instructions sum products of subnormals with errors up to
+// 2^-17 of them.  Element e is nibble kNib[e].
 constexpr int kNib[8] = {0, 4, 1, 5, 2, 6, 3, 7};
 // Masks and exponents as register values the compiler knows nothing of: with literals it takes an and and an or for each
 // pair of codes, from registers the one instruction that does both.
@@ -411,7 +411,9 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
       for (int j = 0; j < TJ; ++j) {
         const v4f k4 = *reinterpret_cast<const v4f*>(&sg.ks[16 * (j0 + j) + 4 * kg]);
         const v4f l4 = *reinterpret_cast<const v4f*>(&sg.ls[16 * (j0 + j) + 4 * kg]);
-        if (ranged) {   // a power of two below 1 goes to the sums, one above 1 comes after the key's scale: no product leaves fp32 before the score does
+        if (ranged) {
+          // a power of two below 1 goes to the sums, one above 1 comes after the key's scale: no product leaves fp32's range
+          // before the score does
 #pragma unroll
           for (int rt = 0; rt < RT; ++rt) {
             const float back = sh.back[16 * rt + c], down = fminf(back, 1.f), up = fmaxf(back, 1.f);
@@ -638,10 +640,10 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
   }
 }
 
-// RT = 1 is bound by its loads: 32 ragged sequences of one token, 154 MB, 43 us with the second launch (3.6 TB/s); 16 chains
-// of 5, 146 MB, 36 us (4.0).  RT = 2 is bound by the instructions a SIMD issues, 544 vector and 112 matrix ones a step of 64
-// tokens: 16 trees of 64 nodes over 8192 tokens 250 us, 0.96 PFLOP/s of matrix instructions.  Two waves to a SIMD: the output
-// sums, weights and the next step's codes take 254 registers.
+// RT = 1 is bound by its loads: 32 ragged sequences of one token, 154 MB, 44 us with the second launch (3.5 TB/s); 16 chains
+// of 5, 146 MB, 37 us (3.9).  RT = 2 is bound by the instructions a SIMD issues, 608 vector and 96 matrix ones a step of 64
+// tokens: 16 trees of 64 nodes over 8192 tokens 264 us, 0.78 PFLOP/s of matrix instructions.  (Times of captured calls on
+// two caches in turn.)  Two waves to a SIMD: the output sums, weights and the next step's codes take 242 registers.
 template <int RT, bool BF16>
 __global__ __launch_bounds__(256, 2) void k_tree(TreeArgs) {
   __shared__ __attribute__((aligned(16))) Tree<RT> sh;

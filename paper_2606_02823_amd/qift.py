@@ -568,7 +568,8 @@ def kv4_attention_tree(q: torch.Tensor, cache: KV4Pages, table: torch.Tensor, st
     taken as they are), sequence b's rows starts[b] .. starts[b+1] - 1 (int32 [B + 1]) being the last of its lens[b]
     cached tokens (int32 [B]) in the pages table[b] (int32 [B, table_pages]).  visible (int64 [rows,
     ceil(max_nodes / 64)]): bit j of a row says that it sees node j of its sequence; None: nodes up to its own.
-    Returns [rows, Hq, 128] in q's type."""
+    Returns [rows, Hq, 128] in q's type; rows behind starts[B] are left as they were in a given out, and hold nothing in
+    particular in a new one."""
     dt, index = q.dtype, cache.index
     if dt not in _HALVES:
         raise TypeError(f"q must be torch.float16 or torch.bfloat16, got {dt}")
