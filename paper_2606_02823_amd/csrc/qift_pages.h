@@ -89,8 +89,8 @@ QIFT_HD uint64_t tree_bits(int32_t d0, uint64_t w0, uint64_t w1) {
 
 // How the attention cuts its work.  A workgroup takes a block of 16 rt query rows (a row is a node and a head of the KV
 // head's group) of one KV head and sequence at a time (a unit), over tokens in rounds of 256: 64 for each of its four
-// waves.  Few units: the rounds of all units, in order, are dealt out evenly to `shares` workgroups a block of rows, whatever the
-// sequences' lengths are; a unit that more than one share covers is joined from partial records.  Beginning and ending a
+// waves.  Few units: the rounds of all units, in order, are dealt out evenly to `shares` workgroups a block of rows, whatever
+// the sequences' lengths are; a unit that more than one share covers is joined from partial records.  Beginning and ending a
 // unit takes a workgroup longer than a round, so a unit is dealt out as its rounds and kBegin more before them (32
 // ragged sequences of 8 heads, where a share may have eight short units: 52 us with 0, 46 with 1, 45 with 2).
 // Many units: one workgroup takes a unit whole, which needs no second launch.  With two workgroups to a CU's place or more
@@ -98,9 +98,9 @@ QIFT_HD uint64_t tree_bits(int32_t d0, uint64_t w0, uint64_t w1) {
 // with half of the places filled where sequences have few rounds (256 blocks, 673 tokens: 17 us, dealt out 24; 448, 1021
 // tokens: 29, 40; 480, 332 tokens: 25, 29).  Below that dealing out wins on ragged sequences (256 units of 32 sequences of
 // up to 8192 tokens: 45 us, whole 63; 280 blocks, 2999 tokens: 37, 39) and loses little on even ones (512 units of 2048
-// tokens: 37.5, 35.2).  The host knows max_len alone, not how the lengths differ, and counts max_nodes for every sequence: from 1024 blocks on
-// one long sequence among short ones, or a chunk's max_nodes beside single tokens, leaves most of the card idle behind a few
-// workgroups (127 sequences of one token, 8 heads, one of 65536 tokens, the others up to 2000: 66 us, dealt out; 128 of
+// tokens: 37.5, 35.2).  The host knows max_len alone, not how the lengths differ, and counts max_nodes for every sequence:
+// from 1024 blocks on one long sequence among short ones, or a chunk's max_nodes beside single tokens, leaves most of the
+// card idle behind a few workgroups (127 sequences of one token, 8 heads, one of 65536 tokens, the others up to 2000: 66 us, dealt out; 128 of
 // them, whole: 420 us.  A chunk of 256 and 3 single tokens, all over 65536: 872 us).
 constexpr int kStep = 64, kWaves = 4, kRound = kStep * kWaves;
 constexpr int kMostShared = 512;   // sequences whose rounds are dealt out (every workgroup adds them up)

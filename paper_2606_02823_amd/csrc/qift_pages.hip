@@ -34,7 +34,8 @@ struct Side {
 // Workgroup (tile, side, head), heads fastest, of 16 tokens, its group of lanes l / 16 the token 16 tile + l / 16.  Bound by
 // its bytes (without its arithmetic it takes as long), and those come best when the heads of a token are read together:
 // 16384 tokens of 8 heads with the values written, 152 MB, 36.7 us with the tiles fastest, 32.1 so (4.7 TB/s; 31.0 us at a
-// large copy's rate; all times here are of captured calls on two caches in turn, so that the Infinity Cache holds neither).  More tiles to a workgroup, their loads ahead, were no faster.
+// large copy's rate; all times here are of captured calls on two caches in turn, so that the Infinity Cache holds neither).
+// More tiles to a workgroup, their loads ahead, were no faster.
 template <bool BF16>
 __global__ __launch_bounds__(256) void k_append(const uint16_t* __restrict__ k, const uint16_t* __restrict__ v,
                                                 int64_t ks, int64_t vs, const int32_t* __restrict__ slots, int n,

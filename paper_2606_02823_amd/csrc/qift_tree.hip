@@ -270,7 +270,9 @@ __device__ __forceinline__ void tree_run(Tree<RT>& sh, const pages::Seq& sq, con
   // offset of the lane.
   uint4 vw[4], kw[4];
   float ksl, vsl;
-  uint8_t kzl, vzl;            // (as words they are extended, and waited for, in the middle of the step before: 43.9 -> 47 us)
+  // (bytes, not words: those would be extended, and all loads waited for, in the middle of the step before; 32 ragged sequences
+  // of one token 47 us instead of 43.9)
+  uint8_t kzl, vzl;
   Rows cur{0, false};
   int32_t ahead = 0;           // the next step's table entry
   const uint32_t koff = 64u * (uint32_t)c + 16u * (uint32_t)kg, voff = 16u * (uint32_t)lane;
