@@ -25,6 +25,10 @@ Modules, each citing the passage it follows:
                            grids of Sec. 3.3)
 * :mod:`oracle.kv4`      - asymmetric 4-bit KV cache and decode attention over it
                            (Sec. 4.1)
+* :mod:`oracle.pages`    - the paged KV4 cache
+* :mod:`oracle.w8`       - the 8-bit linear's quantizers and epilogue
+* :mod:`oracle.step`     - a serving step around the paged cache: tables and slots,
+                           head norms and rotation
 
 Pinned by the ``-m "not gpu"`` tests against the paper's printed constants and
 tables, closed forms, invariants and brute force.  Readings of points where the

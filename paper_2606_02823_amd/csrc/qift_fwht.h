@@ -249,53 +249,57 @@ __device__ __forceinline__ int fwht_tile(double (&v)[E], double* lds, int t, int
   return fwht_tile_s<NT, E, NATURAL>(v, lds, t, L, sync);
 }
 
-// Per-token rounding constants: q = sign(X) min(7, rne(7 den |X| / (num A))).
+// Per-token rounding constants: q = sign(X) min(Q, rne(Q den |X| / (num A))), the largest code Q 7 (INT4) or 127 (INT8).
 struct QuantParams {
   double A;        // max |X| (natural units)
-  double c1;       // 7 den / (num A), fp64 (estimate only)
+  double c1;       // Q den / (num A), fp64 (estimate only)
   int num, den;
 };
 
+template <int Q = 7>
 __device__ __forceinline__ QuantParams make_qparams(double A, int num, int den) {
   QuantParams p;
   p.A = A;
-  p.c1 = A > 0.0 ? (7.0 * den) / ((double)num * A) : 0.0;
+  p.c1 = A > 0.0 ? ((double)Q * den) / ((double)num * A) : 0.0;
   p.num = num;
   p.den = den;
   return p;
 }
 
 // Exact rounding near a half-integer, on the fp64 values |X| <= A taken as rationals:
-// t = 14 den |X| + num A and d = 2 num A, q = floor(t / d), lowered to even on an exact half.
+// t = 2 Q den |X| + num A and d = 2 num A, q = floor(t / d), lowered to even on an exact half.
 // Both are normal doubles (every nonzero rotated value is a sum of fp16 or bf16 values, at
 // least 2^-133): |X| = mx 2^ex, A = ma 2^ea with 53-bit integer mantissas and ea >= ex, so in
-// units of 2^ex, t and d are integers below 2^70 when ea - ex <= 12 (beyond that, 7 den |X| /
-// (num A) < 112 2^-11 and q = 0).  Rarely executed, so it is kept out of line (the inlined
+// units of 2^ex, t and d are integers below 2^75 when ea - ex <= 12, for Q = 127 16 (beyond that, Q den |X| /
+// (num A) < 16 Q 2^-11, 2^-15 and q = 0).  Rarely executed, so it is kept out of line (the inlined
 // copies per element made the kernels larger than the instruction cache).
+template <int Q = 7>
 __device__ __attribute__((noinline)) int quant_exact(double ax, double A, int num, int den, double f) {
-  if (!(f < 8.0)) return 7;   // clamps anyway (and keeps q and t below in range)
+  static_assert(Q == 7 || Q == 127, "the largest code");
+  if (!(f < Q + 1.0)) return Q;   // clamps anyway (and keeps q and t below in range)
   if (!(ax > 0.0)) return 0;
   typedef unsigned __int128 u128;
   const uint64_t bx = (uint64_t)__double_as_longlong(ax), ba = (uint64_t)__double_as_longlong(A);
   const uint64_t mx = (bx & 0xFFFFFFFFFFFFFull) | (1ull << 52), ma = (ba & 0xFFFFFFFFFFFFFull) | (1ull << 52);
   const int s = (int)((ba >> 52) & 0x7FF) - (int)((bx >> 52) & 0x7FF);
-  if (s > 12) return 0;
-  const u128 t = (u128)(14u * (unsigned)den) * mx + (((u128)(unsigned)num * ma) << s);
+  if (s > (Q == 7 ? 12 : 16)) return 0;
+  const u128 t = (u128)(2u * Q * (unsigned)den) * mx + (((u128)(unsigned)num * ma) << s);
   const u128 d = ((u128)(2u * (unsigned)num) * ma) << s;
   int q = (int)f;             // within one of the exact quotient: each loop runs at most twice
   for (int it = 0; it < 4 && q > 0 && (u128)q * d > t; ++it) --q;
   for (int it = 0; it < 4 && (u128)(q + 1) * d <= t; ++it) ++q;
   if ((u128)q * d == t && (q & 1)) --q;
-  return q < 7 ? q : 7;
+  return q < Q ? q : Q;
 }
 
 // Rounding of 16 values.  The fp64 quotient v = X c1 is within 1e-13 of the
-// exact 7 den X / (num A) (|v| <= 112), so unless v lies within 1e-9 of a
+// exact 7 den X / (num A) (|v| <= 112; Q = 127: within 1e-12, |v| <= 2032), so unless v lies within 1e-9 of a
 // half-integer its nearest integer is rint(v); round-half-even is odd-symmetric,
 // so rounding the signed quotient gives sign(X) times the rounded magnitude.
 // That branch-free fast path covers all 16 values; only when some lane of the
 // wave has a value that close to a half (a wave-uniform, rare branch) are those
 // values redone with the exact integer test.
+template <int Q = 7>
 __device__ __forceinline__ void quant16(const double (&v)[16], const QuantParams& p, int (&q)[16]) {
   int near = 0;
 #pragma unroll
@@ -307,7 +311,7 @@ __device__ __forceinline__ void quant16(const double (&v)[16], const QuantParams
     const double tt = vv + 0x1.8p52;
     const double r = tt - 0x1.8p52;
     near |= fabs(vv - r) > 0.5 - 1e-9;
-    q[e] = min(max(__double2loint(tt), -7), 7);   // one v_med3_i32
+    q[e] = min(max(__double2loint(tt), -Q), Q);   // one v_med3_i32
   }
   if (__any(near)) {
 #pragma unroll
@@ -315,7 +319,7 @@ __device__ __forceinline__ void quant16(const double (&v)[16], const QuantParams
       const double ax = fabs(v[e]);
       const double vv = ax * p.c1;
       if (p.A > 0.0 && fabs(vv - rint(vv)) > 0.5 - 1e-9) {
-        const int qq = quant_exact(ax, p.A, p.num, p.den, floor(vv));
+        const int qq = quant_exact<Q>(ax, p.A, p.num, p.den, floor(vv));
         q[e] = v[e] < 0.0 ? -qq : qq;
       }
     }
@@ -429,7 +433,7 @@ __device__ __forceinline__ void unpack16(double (&v)[16], const uint4 (&d)[2]) {
 // Writes the int8 codes (16 per thread per tile, natural order, one 16-byte
 // store) to dst (global or LDS, 16-byte aligned rows) and returns sum_q and
 // the scale.  All NT threads must call it.
-template <int NT, int NTILES, bool BF16 = false>
+template <int NT, int NTILES, bool BF16 = false, int Q = 7>
 __device__ __forceinline__ void quant_token_raw(const TokenRaw<NTILES>& raw, int64_t K, int L, int num, int den,
                                                 double denom, double* lds, double* red_d, int* red_i,
                                                 int8_t* dst, int& sum_q, float& scale) {
@@ -445,13 +449,13 @@ __device__ __forceinline__ void quant_token_raw(const TokenRaw<NTILES>& raw, int
     for (int e = 0; e < 16; ++e) amax = fmax(amax, fabs(v[tau][e]));
   }
   const double A = block_max<NT>(amax, red_d);
-  const QuantParams p = make_qparams(A, num, den);
+  const QuantParams p = make_qparams<Q>(A, num, den);
   int qs = 0;
 #pragma unroll
   for (int tau = 0; tau < NTILES; ++tau) {
     const int64_t base = (int64_t)tau * S::T + 16 * t;
     int q[16];
-    quant16(v[tau], p, q);
+    quant16<Q>(v[tau], p, q);
     uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
@@ -511,7 +515,7 @@ __device__ __forceinline__ void store_codes(int8_t* dst, const int (&q)[16], int
 // exponent L = LC at compile time (every butterfly stage and exchange is then
 // straight-line code); LC = 0 takes L at run time.  With xch0 == xch1 (one
 // exchange buffer) every tile after the first starts with a sync instead.
-template <int NTILES, int LC, bool PLANAR, typename Sync, bool BF16 = false>
+template <int NTILES, int LC, bool PLANAR, typename Sync, bool BF16 = false, int Q = 7>
 __device__ __forceinline__ double quant_token_group(const TokenRaw<NTILES>& raw, int64_t K, int L_rt, int num,
                                                     int den, double* xch0, double* xch1, double* red_d,
                                                     int* red_i, Sync& sync, int8_t* dst, bool xbf16 = false) {
@@ -534,12 +538,12 @@ __device__ __forceinline__ double quant_token_group(const TokenRaw<NTILES>& raw,
   if (lane == 0) red_d[wave] = amax;
   sync();
   const double A = fmax(fmax(red_d[0], red_d[1]), fmax(red_d[2], red_d[3]));
-  const QuantParams p = make_qparams(A, num, den);
+  const QuantParams p = make_qparams<Q>(A, num, den);
   int qs = 0;
 #pragma unroll
   for (int tau = 0; tau < NTILES; ++tau) {
     int q[16];
-    quant16(v[tau], p, q);
+    quant16<Q>(v[tau], p, q);
 #pragma unroll
     for (int e = 0; e < 16; ++e) qs += q[e];
     int8_t* tile_dst = dst + tau * S::T;
@@ -626,13 +630,13 @@ __device__ __forceinline__ double quant_token_wave(const uint4 (&raw)[2], int K,
   return A;
 }
 
-template <int NT, int NTILES, bool BF16 = false>
+template <int NT, int NTILES, bool BF16 = false, int Q = 7>
 __device__ __forceinline__ void quant_token(const uint16_t* xr, int64_t K, int L, int num, int den,
                                             double denom, double* lds, double* red_d, int* red_i,
                                             int8_t* dst, int& sum_q, float& scale) {
   TokenRaw<NTILES> raw;
   load_token_raw<NT, NTILES>(raw, xr, K);
-  quant_token_raw<NT, NTILES, BF16>(raw, K, L, num, den, denom, lds, red_d, red_i, dst, sum_q, scale);
+  quant_token_raw<NT, NTILES, BF16, Q>(raw, K, L, num, den, denom, lds, red_d, red_i, dst, sum_q, scale);
 }
 
 }  // namespace dev

@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "qift_route.h"
+#include "qift_w8_route.h"
 
 namespace qift {
 
@@ -20,6 +21,9 @@ hipError_t launch_pack_w4(const int8_t* levels, int64_t N, int64_t K, uint32_t* 
 constexpr int64_t kWquantMaxK = 16384;
 hipError_t launch_quantize_weights(const float* W, int64_t N, int64_t K, int block, int fmt, int8_t* levels,
                                    uint16_t* scales, hipStream_t s);
+// The same for the 8-bit linear's weights: levels -127..127.
+hipError_t launch_quantize_weights8(const float* W, int64_t N, int64_t K, int block, int8_t* levels, uint16_t* scales,
+                                    hipStream_t s);
 // The same for the mirror family {-1, -r, +r, +1}, 0 < r < 1: codes 0..3 of the ascending levels.
 hipError_t launch_quantize_weights_mirror(const float* W, int64_t N, int64_t K, int block, double r, int8_t* codes,
                                           uint16_t* scales, hipStream_t s);
@@ -72,6 +76,49 @@ struct TreeCall {
   int32_t table_pages, Hq, max_nodes, dtype;
 };
 hipError_t launch_kv4_tree(const TreeCall& a, hipStream_t s);
+// A serving step around the paged cache (qift_step.hip)
+struct PlanCall {
+  const int32_t* lens;
+  const int32_t* counts;
+  int32_t* table;
+  const int32_t* free_pages;
+  const int32_t* free_count;
+  int32_t* starts;
+  int32_t* lens_out;
+  int32_t* slots;
+  int32_t* positions;
+  int32_t* free_out;
+  int64_t B, rows, capacity;   // capacity: entries of free_pages
+  int32_t table_pages, page;
+};
+hipError_t launch_plan_step(const PlanCall& a, hipStream_t s);
+struct ReleaseCall {
+  const int32_t* lens;
+  const int32_t* done;
+  const int32_t* table;
+  int32_t* free_pages;
+  const int32_t* free_count;
+  int32_t* lens_out;
+  int32_t* free_out;
+  int64_t B, capacity;
+  int32_t table_pages, page;
+};
+hipError_t launch_release(const ReleaseCall& a, hipStream_t s);
+// Head norms and position rotation (qift_rope.hip); strides in elements, one entry for queries and one for keys
+struct RopeCall {
+  const uint16_t* x[2];
+  uint16_t* y[2];
+  const uint16_t* weight[2];
+  int64_t x_stride[2], y_stride[2];
+  int32_t heads[2];
+  const int32_t* positions;
+  const float* freq;
+  int64_t rows;
+  float eps;
+  int32_t rot, pairs, dtype;
+};
+hipError_t launch_head_norm_rope(const RopeCall& a, hipStream_t s);
+
 // The status of a HIP call, kept for qift_last_hip_error (qift_api.hip)
 int report_hip(hipError_t e);
 
@@ -84,6 +131,10 @@ hipError_t launch_rotate_quant_act(const uint16_t* x, int64_t M, int64_t K, int 
                                    int clip_den, int8_t* act_q, float* act_scale, int32_t* act_sum,
                                    hipStream_t s, bool bf16 = false);   // x fp16, or bf16 bits
 
+// The same to INT8 (qift_act8.hip), for the 8-bit linear
+hipError_t launch_rotate_quant_act8(const uint16_t* x, int64_t M, int64_t K, int block, int clip_num, int clip_den,
+                                    int8_t* act_q, float* act_scale, hipStream_t s, bool bf16);
+
 // Quantized linear (qift_linear.hip).  fmt selects the decode.  ws (nullable) serves the linears split over
 // K: linear_workspace(fmt, N, M, K) bytes, 0 where the kernel that takes the linear uses none (ws is null then).
 size_t linear_workspace(int fmt, int64_t N, int64_t M, int64_t K);
@@ -94,6 +145,22 @@ hipError_t launch_linear(int fmt, const uint32_t* packed, const uint16_t* scales
 // Tiled GEMM of prompts and of wide linears from 33 tokens on (qift_gemm.hip).
 hipError_t launch_gemm32(int fmt, const uint32_t* P, const uint16_t* sw, int64_t N, int64_t K, const int8_t* act,
                          const float* sx, const int32_t* asum, int64_t M, uint16_t* y, int32_t* acc_out, hipStream_t s);
+
+// The 8-bit linear (qift_w8_rows.hip: up to 64 tokens; qift_w8_gemm.hip); dtype is the outputs' type.
+struct W8Call {
+  const int8_t* levels;
+  const uint16_t* scales;
+  int64_t N, K;
+  const int8_t* act;
+  const float* sx;
+  int64_t M;
+  void* out;
+  int32_t* acc;   // nullable
+  void* ws;       // w8_workspace bytes of the plan
+  int32_t dtype;
+};
+hipError_t launch_w8_rows(const W8Call& c, hipStream_t s);
+hipError_t launch_w8_gemm(const W8Call& c, const route::W8Plan& p, hipStream_t s);
 
 // Linear on codes for batches of up to 64 tokens, K cut into a slice per wave (qift_batch.hip).
 hipError_t launch_batch(int fmt, const uint32_t* P, const uint16_t* sw, int64_t N, int64_t K, const int8_t* act,
@@ -131,8 +198,8 @@ constexpr size_t kReadProbeSegment = 65536;
 size_t read_probe_slots(size_t bytes);
 hipError_t launch_read_probe(const void* buf, size_t bytes, uint32_t* partials, hipStream_t s);
 
-// (den * 7) * sqrt(b): the fixed divisor of the per-token activation scale.
-double act_denominator(int block, int clip_den);
+// (den * Q) * sqrt(b), Q the largest code: the fixed divisor of the per-token activation scale.
+double act_denominator(int block, int clip_den, int largest = 7);
 
 // The per-device error word of the bounded device waits (qift_api.hip): its device address on the
 // current device (nullptr if it cannot be resolved; the kernels then skip the report), and the spin

@@ -1,0 +1,68 @@
+// Arithmetic of a serving step's plan, for the kernels and for host code (plain C++: compiled without a GPU too).
+#pragma once
+
+#include "qift_pages.h"
+
+namespace qift {
+namespace step {
+
+constexpr int kSeqs = 256;   // sequences of a workgroup, one to a thread
+
+// What one sequence asks for, from device data that may hold anything.  room = table_pages * page, below 2^31.
+struct Ask {
+  int32_t len, n;        // cached tokens, brought into [0, room]; new tokens, at least 0
+  int32_t held, need;    // pages that hold the cached tokens; pages to take, 0 for a sequence that cannot be served
+  bool fits, bad;        // its tokens fit its row of the table; one of its numbers is out of range
+};
+QIFT_HD int32_t pages_of(int32_t tokens, pages::Div page) {   // 0 <= tokens < 2^31
+  const uint32_t whole = pages::quotient((uint32_t)tokens, page);
+  return (int32_t)(whole + (whole * page.d != (uint32_t)tokens));
+}
+QIFT_HD Ask ask(int32_t len, int32_t n, int64_t room, pages::Div page) {
+  Ask a;
+  a.bad = len < 0 || (int64_t)len > room || n < 0;
+  const bool len_ok = len >= 0 && (int64_t)len <= room;
+  a.len = len < 0 ? 0 : (int64_t)len > room ? (int32_t)room : len;
+  a.n = n < 0 ? 0 : n;
+  a.fits = len_ok && (int64_t)a.len + a.n <= room;
+  if (!a.fits && a.n > 0) a.bad = true;
+  a.held = pages_of(a.len, page);
+  a.need = a.fits ? pages_of(a.len + a.n, page) - a.held : 0;
+  return a;
+}
+// Whether a sequence has its tokens in this step: start and base are the sums of the new tokens and of the pages that the
+// sequences before it ask for.  Both only grow, so of the sequences that need pages those served are the first ones, and
+// the pages taken are those up to the last one served.
+QIFT_HD bool served(const Ask& a, int64_t start, int64_t base, int64_t rows, int64_t depth) {
+  return a.n > 0 && a.fits && start + a.n <= rows && (a.need == 0 || base + a.need <= depth);
+}
+// Slot of the token at position pos whose page is `entry`; -1 where that is none or the slot has no 31 bits.
+QIFT_HD int32_t slot_of(int32_t entry, uint32_t at, uint32_t page) {
+  const int64_t s = (int64_t)entry * page + at;
+  return entry < 0 || s > 0x7FFFFFFF ? -1 : (int32_t)s;
+}
+// The last of `count` + 1 ascending sums s (s[0] <= at < s[count]) that is at most `at`; a sequence of none is passed over.
+QIFT_HD int32_t find(const int32_t* s, int32_t count, int32_t at) {
+  int32_t lo = 0, hi = count;
+  while (hi - lo > 1) {
+    const int32_t mid = (lo + hi) >> 1;
+    if (s[mid] <= at) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+// Head h of a row's Hq query and Hkv key heads, as a wave takes them four at a time; one past the last is the last again
+// (read, not written), so that it is always a head that is there.
+struct Head {
+  int32_t own;       // among the queries' or the keys'
+  bool have, key;
+};
+QIFT_HD Head head_of(int32_t h, int32_t Hq, int32_t Hkv) {
+  const int32_t all = Hq + Hkv, in = h < all ? h : all - 1;
+  const bool key = in >= Hq;
+  return {key ? in - Hq : in, h < all, key};
+}
+
+}  // namespace step
+}  // namespace qift

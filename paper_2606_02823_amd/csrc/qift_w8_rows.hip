@@ -1,0 +1,112 @@
+// The 8-bit linear for up to 64 tokens: one pass over the weights, K cut into a slice for each wave.
+#include "qift_w8.h"
+
+namespace qift {
+namespace {
+
+using namespace w8;
+
+// A workgroup owns 16 RT weight rows and all the tokens (TT tiles of 16).  Its waves take units of 64 U values of k in turn
+// (unit u is wave u mod NWV's), so that together they read whole pieces of each row; weights and codes go straight to the
+// operands of the 16 x 16 x 64 product (lane (r, g): row or token r, values 16 g .. 16 g + 15 of each 64), the next unit's
+// loads sent before the present one is used.  The waves' sums meet in LDS, each wave adding up and storing some of the tiles.
+// Bound by the weights' bytes.
+template <int RT, int TT, int U, int NWV, int OT>
+__global__ __launch_bounds__(64 * NWV) void k_w8_rows(const int8_t* __restrict__ W, const uint16_t* __restrict__ sw, int64_t N,
+                                                      int K, const int8_t* __restrict__ act, const float* __restrict__ sx,
+                                                      int M, void* __restrict__ y, int32_t* __restrict__ acc_out) {
+  __shared__ __align__(16) v4i part[NWV][RT * TT][64];
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t n_base = (int64_t)blockIdx.x * (16 * RT);
+  const int rows = (int)(N - n_base < 16 * RT ? N - n_base : 16 * RT);
+  const __amdgpu_buffer_rsrc_t wr = dev::make_rsrc(W + n_base * K, (uint32_t)rows * (uint32_t)K);
+  const __amdgpu_buffer_rsrc_t ar = dev::make_rsrc(act, (uint32_t)M * (uint32_t)K);
+  uint32_t wo[RT], ao[TT];
+#pragma unroll
+  for (int j = 0; j < RT; ++j) wo[j] = 16 * j + r < rows ? (uint32_t)(16 * j + r) * (uint32_t)K + 16u * g : dev::kOutOfRange;
+#pragma unroll
+  for (int t = 0; t < TT; ++t) ao[t] = 16 * t + r < M ? (uint32_t)(16 * t + r) * (uint32_t)K + 16u * g : dev::kOutOfRange;
+  struct Unit {
+    uint4 w[U][RT], a[U][TT];
+  };
+  // (K is a multiple of 64: what lies past it is out of range in whole 64s)
+  auto load = [&](Unit& b, int k) {
+#pragma unroll
+    for (int s = 0; s < U; ++s) {
+      const bool in = k + 64 * s < K;
+#pragma unroll
+      for (int j = 0; j < RT; ++j) b.w[s][j] = dev::bload16(wr, in ? wo[j] + (uint32_t)(k + 64 * s) : dev::kOutOfRange);
+#pragma unroll
+      for (int t = 0; t < TT; ++t) b.a[s][t] = dev::bload16(ar, in ? ao[t] + (uint32_t)(k + 64 * s) : dev::kOutOfRange);
+    }
+  };
+  v4i acc[RT][TT];
+#pragma unroll
+  for (int j = 0; j < RT; ++j)
+#pragma unroll
+    for (int t = 0; t < TT; ++t) acc[j][t] = v4i{0, 0, 0, 0};
+  auto use = [&](const Unit& b) {
+#pragma unroll
+    for (int s = 0; s < U; ++s)
+#pragma unroll
+      for (int j = 0; j < RT; ++j)
+#pragma unroll
+        for (int t = 0; t < TT; ++t)
+          acc[j][t] = mma::mfma_i8(v4i{(int)b.w[s][j].x, (int)b.w[s][j].y, (int)b.w[s][j].z, (int)b.w[s][j].w},
+                                   v4i{(int)b.a[s][t].x, (int)b.a[s][t].y, (int)b.a[s][t].z, (int)b.a[s][t].w}, acc[j][t]);
+  };
+  constexpr int kStride = 64 * U * NWV;
+  Unit u0, u1;
+  int k = 64 * U * wave;
+  load(u0, k);
+  for (; k < K; k += 2 * kStride) {
+    load(u1, k + kStride);
+    use(u0);
+    load(u0, k + 2 * kStride);
+    use(u1);
+  }
+#pragma unroll
+  for (int j = 0; j < RT; ++j)
+#pragma unroll
+    for (int t = 0; t < TT; ++t) part[wave][j * TT + t][lane] = acc[j][t];
+  __syncthreads();
+  for (int p = wave; p < RT * TT; p += NWV) {
+    v4i d = part[0][p][lane];
+#pragma unroll
+    for (int w = 1; w < NWV; ++w) d += part[w][p][lane];
+    const int j = p / TT, t = p - j * TT, m = 16 * t + r;
+    const int64_t n0 = n_base + 16 * j + 4 * g;
+    if (m >= M || n0 >= N) continue;
+    const int a[4] = {d[0], d[1], d[2], d[3]};
+    float s4[4];
+    scales4(load_scales(sw, n0, N), s4);
+    store_quad<OT>(y, m, n0, N, quad<OT>(a, sx[m], s4));
+    if (acc_out) store_quad<kAcc>(acc_out, m, n0, N, quad<kAcc>(a, 0.f, s4));
+  }
+}
+
+template <int RT, int TT, int U, int NWV>
+hipError_t launch_rows(const W8Call& c, hipStream_t s) {
+  const dim3 grid((unsigned)((c.N + 16 * RT - 1) / (16 * RT)));
+  auto kernel = c.dtype == kF32    ? k_w8_rows<RT, TT, U, NWV, kF32>
+                : c.dtype == kBF16 ? k_w8_rows<RT, TT, U, NWV, kBF16>
+                                   : k_w8_rows<RT, TT, U, NWV, kF16>;
+  hipLaunchKernelGGL(kernel, grid, dim3(64 * NWV), 0, s, c.levels, c.scales, c.N, (int)c.K, c.act, c.sx, (int)c.M, c.out,
+                     c.acc);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_w8_rows(const W8Call& c, hipStream_t s) {
+  const int tt = (int)((c.M + 15) / 16);
+  // 16 rows to a workgroup while that gives fewer than two workgroups to a CU, else 32, with more tokens 64
+  const int64_t tiles = (c.N + 15) / 16;
+  if (tt == 1) return tiles <= 512 ? launch_rows<1, 1, 4, 8>(c, s) : launch_rows<2, 1, 4, 8>(c, s);
+  if (tt == 2) return tiles <= 512 ? launch_rows<1, 2, 4, 8>(c, s) : tiles <= 1024 ? launch_rows<2, 2, 2, 8>(c, s) : launch_rows<4, 2, 2, 4>(c, s);
+  if (tt == 3) return tiles <= 512 ? launch_rows<1, 3, 2, 8>(c, s) : tiles <= 1024 ? launch_rows<2, 3, 2, 8>(c, s) : launch_rows<4, 3, 2, 4>(c, s);
+  return tiles <= 512 ? launch_rows<1, 4, 2, 8>(c, s) : tiles <= 1024 ? launch_rows<2, 4, 2, 8>(c, s) : launch_rows<4, 4, 2, 4>(c, s);
+}
+
+}  // namespace qift

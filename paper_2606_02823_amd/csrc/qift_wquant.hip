@@ -10,11 +10,12 @@
 //        linspace(0.2, 1, 64) * max|row| / 4, of sum (w - s * level(w, s))^2,
 //        level in {-4,-1,+1,+4} by |u| > 5/2 (Eq. (17));
 //   W4   s_w = fp16(max|row| / 7), q = clip(rne(w / s_w), -7, 7) (Eq. (1));
+//   W8   the same with 127;
 //   G(r) the mirror family {-1, -r, +r, +1} (Sec. 3.4 Eq. (18)) with the PoT scale search (outer
 //        level 1: candidates linspace(0.2, 1, 64) * max|row|), the outer level where |u| > (1 + r) / 2;
 //        written as codes 0..3 of the ascending levels (the level-table linear's input).
 // Readings: a value on a midpoint takes the inner level, zero the positive one;
-// a row whose stored scale is 0 gets level +1 (W2) or 0 (W4).
+// a row whose stored scale is 0 gets level +1 (W2) or 0 (W4, W8).
 //
 // One 256-thread workgroup per row; thread t holds elements 16 t .. 16 t + 15
 // of every 4096-element tile in fp64 registers, rotated with the butterfly
@@ -40,6 +41,11 @@ using mma::FMT_W4;
 namespace {
 
 constexpr int FMT_MIRROR = 3;   // G(r): a run-time inner level r, codes out
+constexpr int FMT_W8 = 5;       // the 8-bit linear's weights
+template <int FMT>
+constexpr bool is_sym() { return FMT == FMT_W4 || FMT == FMT_W8; }   // symmetric integers -Q .. Q
+template <int FMT>
+constexpr double largest() { return FMT == FMT_W8 ? 127.0 : 7.0; }
 
 // fp64 -> IEEE binary16 bits, round to nearest, ties to even, overflow to infinity (from the bit
 // fields: 10 fraction bits kept, the rest rounded; below 2^-14 in units of 2^-24).
@@ -182,13 +188,13 @@ __global__ __launch_bounds__(256) void k_quant_weights(const float* __restrict__
       for (int e = 0; e < 16; ++e) ss += v[tau][e] * v[tau][e];
     const double s = sqrt(group_sum(ss, xch) / (double)K);
     sw = half_bits_rne(s / 2.0);
-  } else if constexpr (FMT == FMT_W4) {
+  } else if constexpr (is_sym<FMT>()) {
     amax = dev::wave_max(amax);
     __syncthreads();
     if (lane == 0) xch[red_slot(wave)] = amax;
     __syncthreads();
     const double a = max_of_slots(xch);
-    sw = half_bits_rne(a / 7.0);
+    sw = half_bits_rne(a / largest<FMT>());
   } else {
     amax = dev::wave_max(amax);
     __syncthreads();
@@ -293,7 +299,7 @@ __global__ __launch_bounds__(256) void k_quant_weights(const float* __restrict__
   if (t == 0) scales[n] = sw;
 
   // ---- levels against the stored scale, decided as by the rounded quotient u = w / s_w:
-  //   MNZ |u| > 2 -> 3, PoT |u| > 2.5 -> 4 (else 1, sign of w), W4 q = clamp(rint(u), -7, 7).
+  //   MNZ |u| > 2 -> 3, PoT |u| > 2.5 -> 4 (else 1, sign of w), W4 and W8 q = clamp(rint(u), -Q, Q).
   // Without the division where the decision is clear: for the two-level sets the exact sign of
   // fma(-thr, s_w, |w|) (the quotient and the real ratio can disagree only within 2^-51 s_w above
   // the threshold); for W4 the product with 1/s_w rounded to q0, kept when the residual w - q0 s_w
@@ -309,10 +315,10 @@ __global__ __launch_bounds__(256) void k_quant_weights(const float* __restrict__
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       const double w = v[tau][e];
-      if constexpr (FMT == FMT_W4) {
+      if constexpr (is_sym<FMT>()) {
         const double q0 = rint(w * inv_sw);
         const double res = fma(-q0, s_w, w);
-        q[e] = (int)fmin(fmax(q0, -7.0), 7.0);
+        q[e] = (int)fmin(fmax(q0, -largest<FMT>()), largest<FMT>());
         nr |= (uint32_t)(fabs(res) >= (0.5 - 0x1p-45) * s_w) << e;
       } else {
         const double r = fma(-thr, s_w, fabs(w));
@@ -326,8 +332,8 @@ __global__ __launch_bounds__(256) void k_quant_weights(const float* __restrict__
         for (int e = 0; e < 16; ++e) {
           if ((nr >> e) & 1u) {
             const double u = v[tau][e] / s_w;
-            if constexpr (FMT == FMT_W4) {
-              q[e] = (int)fmin(fmax(rint(u), -7.0), 7.0);
+            if constexpr (is_sym<FMT>()) {
+              q[e] = (int)fmin(fmax(rint(u), -largest<FMT>()), largest<FMT>());
             } else {
               q[e] = level_of<FMT>(u >= 0.0, fabs(u) > thr);
             }
@@ -336,7 +342,7 @@ __global__ __launch_bounds__(256) void k_quant_weights(const float* __restrict__
       }
     } else {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) q[e] = FMT == FMT_W4 ? 0 : FMT == FMT_MIRROR ? 2 : 1;
+      for (int e = 0; e < 16; ++e) q[e] = is_sym<FMT>() ? 0 : FMT == FMT_MIRROR ? 2 : 1;
     }
     uint32_t wd[4] = {0, 0, 0, 0};
 #pragma unroll
@@ -390,6 +396,11 @@ hipError_t launch_quantize_weights(const float* W, int64_t N, int64_t K, int blo
     case FMT_W4: return launch_fmt<FMT_W4>(W, N, K, L, sqrtb, 0.0, levels, scales, s);
     default: return hipErrorInvalidValue;
   }
+}
+
+hipError_t launch_quantize_weights8(const float* W, int64_t N, int64_t K, int block, int8_t* levels, uint16_t* scales,
+                                    hipStream_t s) {
+  return launch_fmt<FMT_W8>(W, N, K, dev::ilog2c(block), sqrt((double)block), 0.0, levels, scales, s);
 }
 
 hipError_t launch_quantize_weights_mirror(const float* W, int64_t N, int64_t K, int block, double r, int8_t* codes,

@@ -2,7 +2,7 @@
 
 Every function here checks tensor dtypes, shapes and devices, passes raw
 device pointers and the current HIP stream to the C ABI declared in
-``include/qift.h``, and raises on a non-zero status.  All arithmetic happens
+``include/qift.h`` (and ``qift_pages.h``, ``qift_w8.h``, ``qift_step.h``), and raises on a non-zero status.  All arithmetic happens
 in the library's HIP kernels; there is no fallback path.  PyTorch serves only
 for device memory and streams.
 
@@ -41,6 +41,12 @@ EXPORTS = ("qift_packed_bytes", "qift_pack_w2", "qift_pack_w4", "qift_quantize_w
 
 # every symbol declared in include/qift_pages.h
 PAGES_EXPORTS = ("qift_kv4_append", "qift_kv4_read", "qift_kv4_attention_tree_workspace_bytes", "qift_kv4_attention_tree")
+
+# every symbol declared in include/qift_w8.h
+W8_EXPORTS = ("qift_quantize_weights8", "qift_rotate_quant_act8", "qift_w8a8_workspace_bytes", "qift_w8a8_linear")
+
+# every symbol declared in include/qift_step.h
+STEP_EXPORTS = ("qift_kv4_plan_step", "qift_kv4_release", "qift_head_norm_rope")
 
 
 class QiftError(RuntimeError):
@@ -94,6 +100,15 @@ class KV4PagesC(ctypes.Structure):
                 ("v_zeros", ctypes.c_void_p)]
 
 
+class W8C(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int64), ("K", ctypes.c_int64), ("levels", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
+
+
+class HeadRopeC(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("rot", ctypes.c_int32), ("pairs", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("freq", ctypes.c_void_p), ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p)]
+
+
 _lib = None
 
 
@@ -144,6 +159,13 @@ def lib():
         "qift_kv4_attention_tree_workspace_bytes": (sz, [i64, i32, i32, i32, i32, i64]),
         "qift_kv4_attention_tree": (ctypes.c_int, [vp, vp, i64, i32, i64, vp, i32, vp, vp, i64, i32, i32, i64, vp, vp, vp,
                                                    sz, vp]),
+        "qift_quantize_weights8": (ctypes.c_int, [vp, i64, HadamardSpec, vp, vp, vp]),
+        "qift_rotate_quant_act8": (ctypes.c_int, [vp, i64, HadamardSpec, vp, vp, vp]),
+        "qift_w8a8_workspace_bytes": (sz, [vp, i64]),
+        "qift_w8a8_linear": (ctypes.c_int, [vp, vp, vp, i64, i32, vp, vp, vp, sz, vp]),
+        "qift_kv4_plan_step": (ctypes.c_int, [vp, vp, i64, vp, i32, i32, vp, vp, i64, i64, vp, vp, vp, vp, vp, vp]),
+        "qift_kv4_release": (ctypes.c_int, [vp, vp, i64, vp, i32, i32, vp, vp, i64, vp, vp, vp]),
+        "qift_head_norm_rope": (ctypes.c_int, [vp, vp, i64, vp, i64, i32, vp, i64, i32, i32, vp, i64, vp, i64, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -469,41 +491,41 @@ def _empty_pair(shape, dtype, device, stream=None):
 _HALVES = (torch.float16, torch.bfloat16)
 
 
-# The checks of the paged calls, each one expression where all is well (a decode step's append runs 3 us on the GPU):
+# The checks of the paged calls, of a step's and of the 8-bit linear's, each one expression where all is well (a decode step's append runs 3 us on the GPU):
 # tensors on the cache's device, of the type and shape; what is wrong is said where an expression fails.
-def _on_device(t, index, name):
+def _on_device(t, index, name, of="cache"):
     if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
         raise TypeError(f"{name} must be a CUDA (HIP) tensor")
     if t.get_device() != index:
-        raise ValueError(f"{name} is on {t.device}, the cache on device {index}")
+        raise ValueError(f"{name} is on {t.device}, the {of} on device {index}")
 
 
-def _dense(t, index, dtype, shape, name):
+def _dense(t, index, dtype, shape, name, of="cache"):
     if t.__class__ is torch.Tensor and t.get_device() == index and t.dtype is dtype and t.shape == shape and t.is_contiguous():
         return
-    _on_device(t, index, name)
+    _on_device(t, index, name, of)
     _dev(t, dtype, shape, name)
 
 
-def _rows(t, index, dtype, shape, name) -> int:
+def _rows(t, index, dtype, shape, name, of="cache") -> int:
     """The row stride of a [rows, heads, 128] view whose rows are contiguous (a part of stacked rows, say)."""
     if not (t.__class__ is torch.Tensor and t.get_device() == index and t.dtype is dtype and t.shape == shape):
-        _on_device(t, index, name)
+        _on_device(t, index, name, of)
         if t.dtype != dtype:
             raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
         if tuple(t.shape) != tuple(shape):
             raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     n, heads = shape[0], shape[1]
     row, head, one = t.stride()
-    if (one != 1 or (head != 128 and heads > 1)) and n:
+    if (one != 1 or (head != 128 and heads > 1)) and n and heads:
         raise ValueError(f"{name} must have contiguous rows")
     return row if n > 1 else heads * 128
 
 
-def _run(index, call, args, stream):
+def _run(index, call, args, stream, of="cache"):
     """The call on its device (kernels are launched on the current device and its current stream)."""
     if stream is not None and getattr(stream, "device_index", index) != index:
-        raise ValueError(f"the stream is on device {stream.device_index}, the cache on device {index}")
+        raise ValueError(f"the stream is on device {stream.device_index}, the {of} on device {index}")
     if (_raw_device() if _raw_device is not None else torch.cuda.current_device()) == index:
         return call(*args, _stream(stream))
     with torch.cuda.device(index):
@@ -602,6 +624,129 @@ def kv4_attention_tree(q: torch.Tensor, cache: KV4Pages, table: torch.Tensor, st
     return out
 
 
+@dataclass
+class KV4Plan:
+    """Where the new tokens of a step go (kv4_plan_step), all int32: starts [B + 1], lens [B] with the new tokens, slots and
+    positions [rows], free_count [1] of the stack after the step.  lens and free_count are the next step's inputs."""
+    starts: torch.Tensor
+    lens: torch.Tensor
+    slots: torch.Tensor
+    positions: torch.Tensor
+    free_count: torch.Tensor
+
+
+def _step_tables(lens, table, free_pages, free_count):
+    if table.dim() != 2 or free_pages.dim() != 1:
+        raise ValueError(f"table must have shape (B, table_pages), free_pages (capacity,); got {tuple(table.shape)}, "
+                         f"{tuple(free_pages.shape)}")
+    B, width = table.shape
+    index = table.get_device()
+    _dense(table, index, torch.int32, (B, width), "table", "table")
+    _dense(lens, index, torch.int32, (B,), "lens", "table")
+    _dense(free_pages, index, torch.int32, free_pages.shape, "free_pages", "table")
+    _dense(free_count, index, torch.int32, (1,), "free_count", "table")
+    return B, width, index
+
+
+def kv4_plan_step(lens: torch.Tensor, counts: torch.Tensor, table: torch.Tensor, free_pages: torch.Tensor,
+                  free_count: torch.Tensor, page: int, rows: int, out: KV4Plan | None = None, stream=None) -> KV4Plan:
+    """Slots, positions, row starts and new lengths of counts[b] new tokens for each of B sequences with lens[b] cached
+    ones (int32 [B]), their pages taken from the top of the stack free_pages[: free_count] (int32 [capacity], [1]) into
+    table (int32 [B, table_pages], written in place).  rows: how many rows the step has room for.  What out names must be
+    other tensors than lens and free_count."""
+    B, width, index = _step_tables(lens, table, free_pages, free_count)
+    _dense(counts, index, torch.int32, (B,), "counts", "table")
+    if out is None:   # one piece of memory for the five
+        out = KV4Plan(*_empty((2 * B + 2 * rows + 2,), torch.int32, table.device, stream).split((B + 1, B, rows, rows, 1)))
+    else:
+        _dense(out.starts, index, torch.int32, (B + 1,), "starts", "table")
+        _dense(out.lens, index, torch.int32, (B,), "lens", "table")
+        _dense(out.slots, index, torch.int32, (rows,), "slots", "table")
+        _dense(out.positions, index, torch.int32, (rows,), "positions", "table")
+        _dense(out.free_count, index, torch.int32, (1,), "free_count", "table")
+    st = _run(index, lib().qift_kv4_plan_step,
+              (lens.data_ptr(), counts.data_ptr(), B, table.data_ptr(), width, page, free_pages.data_ptr(), free_count.data_ptr(),
+               free_pages.shape[0], rows, out.starts.data_ptr(), out.lens.data_ptr(), out.slots.data_ptr(),
+               out.positions.data_ptr(), out.free_count.data_ptr()), stream, "table")
+    if st:
+        _check("qift_kv4_plan_step", st)
+    return out
+
+
+def kv4_release(lens: torch.Tensor, done: torch.Tensor, table: torch.Tensor, free_pages: torch.Tensor, free_count: torch.Tensor,
+                page: int, out=None, stream=None):
+    """The pages of the sequences with done[b] != 0 (int32 [B]) put back on the stack (free_pages, written in place).
+    Returns (lens, free_count) after that, new tensors or the pair out."""
+    B, width, index = _step_tables(lens, table, free_pages, free_count)
+    _dense(done, index, torch.int32, (B,), "done", "table")
+    if out is None:
+        out = _empty((B + 1,), torch.int32, table.device, stream).split((B, 1))
+    lens_out, free_out = out
+    _dense(lens_out, index, torch.int32, (B,), "lens", "table")
+    _dense(free_out, index, torch.int32, (1,), "free_count", "table")
+    st = _run(index, lib().qift_kv4_release,
+              (lens.data_ptr(), done.data_ptr(), B, table.data_ptr(), width, page, free_pages.data_ptr(), free_count.data_ptr(),
+               free_pages.shape[0], lens_out.data_ptr(), free_out.data_ptr()), stream, "table")
+    if st:
+        _check("qift_kv4_release", st)
+    return lens_out, free_out
+
+
+class HeadRope:
+    """Norms and rotation of a model's heads (qift_head_rope): freq fp32 [rot / 2], the weights [128] in the rows' type or
+    None (not normed); pairs: values 2 i and 2 i + 1 are paired, else i and i + rot / 2.  The object keeps the tensors alive and
+    holds the C view, checked once here."""
+
+    def __init__(self, freq: torch.Tensor, rot: int = 128, pairs: bool = False, q_weight: torch.Tensor | None = None,
+                 k_weight: torch.Tensor | None = None, eps: float = 1e-5):
+        _dev(freq, torch.float32, (rot // 2,), "freq")
+        self.device, self.index = freq.device, freq.get_device()
+        self.dtype = None   # of the weights
+        for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+            if w is None:
+                continue
+            if w.dtype not in _HALVES:
+                raise TypeError(f"{name} must be torch.float16 or torch.bfloat16, got {w.dtype}")
+            if self.dtype is not None and w.dtype != self.dtype:
+                raise TypeError(f"k_weight must be {self.dtype}, got {w.dtype}")
+            self.dtype = w.dtype
+            _dense(w, self.index, w.dtype, (128,), name, "frequencies")
+        self.freq, self.q_weight, self.k_weight = freq, q_weight, k_weight
+        self.c = HeadRopeC(128, rot, int(pairs), eps, freq.data_ptr(), _ptr(q_weight), _ptr(k_weight))
+        self._ref = ctypes.byref(self.c)
+
+
+def head_norm_rope(rope: HeadRope, q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, out=None, stream=None):
+    """Norm of each head of the queries q [rows, Hq, 128] and keys k [rows, Hkv, 128] (fp16 or bf16, row-strided views taken
+    as they are) and its rotation by positions (int32 [rows]; negative: padding, zeros).  out: a pair of such views to write,
+    q and k themselves among what is taken.  Returns (q, k)."""
+    dt, index = q.dtype, rope.index
+    if dt not in _HALVES:
+        raise TypeError(f"q must be torch.float16 or torch.bfloat16, got {dt}")
+    if rope.dtype is not None and dt is not rope.dtype:
+        raise TypeError(f"q must have the norms' type {rope.dtype}, got {dt}")
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError(f"q and k must have shape (rows, heads, 128), got {tuple(q.shape)}, {tuple(k.shape)}")
+    rows, Hq, _ = q.shape
+    Hkv = k.shape[1]
+    qs = _rows(q, index, dt, (rows, Hq, 128), "q", "frequencies")
+    ks = _rows(k, index, dt, (rows, Hkv, 128), "k", "frequencies")
+    _dense(positions, index, torch.int32, (rows,), "positions", "frequencies")
+    if out is None:
+        qo, ko = _empty((rows, Hq, 128), dt, q.device, stream), _empty((rows, Hkv, 128), dt, q.device, stream)
+        qos, kos = Hq * 128, Hkv * 128
+    else:
+        qo, ko = out
+        qos = _rows(qo, index, dt, (rows, Hq, 128), "out", "frequencies")
+        kos = _rows(ko, index, dt, (rows, Hkv, 128), "out", "frequencies")
+    st = _run(index, lib().qift_head_norm_rope,
+              (rope._ref, q.data_ptr(), qs, k.data_ptr(), ks, _DTYPE[dt], positions.data_ptr(), rows, Hq, Hkv, qo.data_ptr(), qos,
+               ko.data_ptr(), kos), stream, "frequencies")
+    if st:
+        _check("qift_head_norm_rope", st)
+    return qo, ko
+
+
 def rotate_quant_act(x: torch.Tensor, block: int, clip=(1, 1), out: QAct | None = None, stream=None) -> QAct:
     """Exact block-Hadamard rotation + per-token INT4 quantization of fp16 or bf16 x [M, K]."""
     M, K = x.shape
@@ -683,8 +828,118 @@ def w4a4_linear(w: Packed, act: QAct, out=None, acc_out=None, workspace=None, us
     return _linear("qift_w4a4_linear", w, act, out, acc_out, workspace, use_sum, stream)
 
 
-def linear(w: Packed, act: QAct, out=None, acc_out=None, workspace=None, use_sum=False, stream=None) -> torch.Tensor:
-    """Dispatch on the weight format."""
+class W8:
+    """8-bit weights (qift_w8): levels int8 [N, K], scales fp16 [N].  The object keeps the tensors alive and holds the C
+    view, checked once here."""
+
+    def __init__(self, levels: torch.Tensor, scales: torch.Tensor):
+        if levels.dim() != 2:
+            raise ValueError(f"levels must have shape (N, K), got {tuple(levels.shape)}")
+        self.N, self.K = levels.shape
+        _dev(levels, torch.int8, (self.N, self.K), "levels")
+        _dev(scales, torch.float16, (self.N,), "scales")
+        if levels.device != scales.device:
+            raise ValueError(f"the weights' tensors are on {levels.device} and {scales.device}")
+        self.levels, self.scales = levels, scales
+        self.device, self.index = levels.device, levels.get_device()
+        self.c = W8C(self.N, self.K, levels.data_ptr(), scales.data_ptr())
+        self._ref = ctypes.byref(self.c)
+
+    @property
+    def nbytes(self) -> int:
+        return self.levels.numel()
+
+
+def quantize_weights8(W: torch.Tensor, block: int, levels: torch.Tensor | None = None, scales: torch.Tensor | None = None,
+                      stream=None) -> W8:
+    """Rotate the rows of fp32 W [N, K] by the block Hadamard and quantize them to 8 bits with an absmax / 127 scale each
+    (levels int8 [N, K], scales fp16 [N]: new, or those given)."""
+    N, K = W.shape
+    _dev(W, torch.float32, (N, K), "W")
+    index = W.get_device()
+    if levels is None:
+        levels = _empty((N, K), torch.int8, W.device, stream)
+    if scales is None:
+        scales = _empty((N,), torch.float16, W.device, stream)
+    _dense(levels, index, torch.int8, (N, K), "levels", "W")
+    _dense(scales, index, torch.float16, (N,), "scales", "W")
+    st = _run(index, lib().qift_quantize_weights8, (W.data_ptr(), N, spec(K, block), levels.data_ptr(), scales.data_ptr()),
+              stream, "W")
+    if st:
+        _check("qift_quantize_weights8", st)
+    return W8(levels, scales)
+
+
+def alloc_act8(M: int, K: int, device="cuda", stream=None) -> QAct:
+    """Codes and scales of M tokens for the 8-bit linear (no code sums: its operands are the levels themselves)."""
+    return QAct(_empty((M, K), torch.int8, device, stream), _empty((M,), torch.float32, device, stream))
+
+
+def rotate_quant_act8(x: torch.Tensor, block: int, clip=(1, 1), out: QAct | None = None, stream=None) -> QAct:
+    """Exact block-Hadamard rotation + per-token INT8 quantization of fp16 or bf16 x [M, K]."""
+    dt = x.dtype
+    if dt not in _HALVES:
+        raise TypeError(f"x must be torch.float16 or torch.bfloat16, got {dt}")
+    M, K = x.shape
+    _dev(x, dt, (M, K), "x")
+    index = x.get_device()
+    if out is None:
+        out = alloc_act8(M, K, x.device, stream)
+    _dense(out.q, index, torch.int8, (M, K), "act_q", "x")
+    _dense(out.scale, index, torch.float32, (M,), "act_scale", "x")
+    st = _run(index, lib().qift_rotate_quant_act8, (x.data_ptr(), M, spec(K, block, clip, dt is torch.bfloat16),
+                                                    out.q.data_ptr(), out.scale.data_ptr()), stream, "x")
+    if st:
+        _check("qift_rotate_quant_act8", st)
+    return out
+
+
+def w8a8_workspace_bytes(w: W8, M: int) -> int:
+    return int(lib().qift_w8a8_workspace_bytes(w._ref, M))
+
+
+def w8a8_workspace(w: W8, M: int, stream=None) -> torch.Tensor | None:
+    """A workspace for w8a8_linear calls with these weights and M tokens (one call at a time); None where it needs none."""
+    need = w8a8_workspace_bytes(w, M)
+    return _empty((need,), torch.uint8, w.device, stream) if need else None
+
+
+def w8a8_linear(w: W8, act: QAct, dtype=torch.float16, out=None, acc_out=None, workspace=None, stream=None) -> torch.Tensor:
+    """y [M, N] of the 8-bit linear in dtype fp16, bf16 or fp32 (the type of out, if that is given); acc_out receives the
+    int32 sums.  Without a workspace K is not cut."""
+    index = w.index
+    if act.q.dim() != 2 or act.q.shape[1] != w.K:
+        raise ValueError(f"activation codes must have shape (M, {w.K}), got {tuple(act.q.shape)}")
+    M = act.q.shape[0]
+    _dense(act.q, index, torch.int8, (M, w.K), "act_q", "weights")
+    _dense(act.scale, index, torch.float32, (M,), "act_scale", "weights")
+    if out is not None:
+        dtype = out.dtype
+    if dtype not in _DTYPE:
+        raise TypeError(f"dtype must be torch.float16, torch.bfloat16 or torch.float32, got {dtype}")
+    if out is None:
+        out = _empty((M, w.N), dtype, w.device, stream)
+    else:
+        _dense(out, index, dtype, (M, w.N), "out", "weights")
+    if acc_out is not None:
+        _dense(acc_out, index, torch.int32, (M, w.N), "acc_out", "weights")
+    ws_bytes = 0
+    if workspace is not None:
+        ws_bytes = workspace.numel()
+        _dense(workspace, index, torch.uint8, (ws_bytes,), "workspace", "weights")
+    st = _run(index, lib().qift_w8a8_linear, (w._ref, act.q.data_ptr(), act.scale.data_ptr(), M, _DTYPE[dtype], out.data_ptr(),
+                                              _ptr(acc_out), _ptr(workspace), ws_bytes), stream, "weights")
+    if st:
+        _check("qift_w8a8_linear", st)
+    return out
+
+
+def linear(w: Packed | W8, act: QAct, out=None, acc_out=None, workspace=None, use_sum=False, stream=None) -> torch.Tensor:
+    """Dispatch on the weight format (8-bit weights take the codes of rotate_quant_act8)."""
+    if isinstance(w, W8):
+        if use_sum:
+            raise ValueError("the 8-bit linear takes no code sums")
+        return w8a8_linear(w, act, out=out, acc_out=acc_out, workspace=workspace, stream=stream)
     f = w4a4_linear if w.fmt == W4_SYM else w2a4_linear
     return f(w, act, out=out, acc_out=acc_out, workspace=workspace, use_sum=use_sum, stream=stream)
 
