@@ -146,7 +146,7 @@ hipError_t launch_linear(int fmt, const uint32_t* packed, const uint16_t* scales
 hipError_t launch_gemm32(int fmt, const uint32_t* P, const uint16_t* sw, int64_t N, int64_t K, const int8_t* act,
                          const float* sx, const int32_t* asum, int64_t M, uint16_t* y, int32_t* acc_out, hipStream_t s);
 
-// The 8-bit linear (qift_w8_rows.hip: up to 64 tokens; qift_w8_gemm.hip); dtype is the outputs' type.
+// The 8-bit linear (qift_w8_rows.hip, qift_w8_gemm.hip; which: qift_w8_route.h); dtype is the outputs' type.
 struct W8Call {
   const int8_t* levels;
   const uint16_t* scales;
@@ -159,7 +159,7 @@ struct W8Call {
   void* ws;       // w8_workspace bytes of the plan
   int32_t dtype;
 };
-hipError_t launch_w8_rows(const W8Call& c, hipStream_t s);
+hipError_t launch_w8_rows(const W8Call& c, const route::W8Plan& p, hipStream_t s);
 hipError_t launch_w8_gemm(const W8Call& c, const route::W8Plan& p, hipStream_t s);
 
 // Linear on codes for batches of up to 64 tokens, K cut into a slice per wave (qift_batch.hip).

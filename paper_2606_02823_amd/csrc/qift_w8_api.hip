@@ -52,7 +52,7 @@ int qift_rotate_quant_act8(const uint16_t* x, int64_t M, qift_hadamard_spec spec
 }
 
 size_t qift_w8a8_workspace_bytes(const qift_w8* w, int64_t M) {
-  return w && shape_ok(w->N, w->K, M) ? qift::route::w8_workspace(w->N, M, w->K) : 0;
+  return w && shape_ok(w->N, w->K, M) ? qift::route::w8_workspace(qift::route::w8_plan(w->N, M, w->K, true), w->N, M) : 0;
 }
 
 int qift_w8a8_linear(const qift_w8* w, const int8_t* act_q, const float* act_scale, int64_t M, int32_t dtype, void* out,
@@ -60,18 +60,15 @@ int qift_w8a8_linear(const qift_w8* w, const int8_t* act_q, const float* act_sca
   if (!w || !w->levels || !w->scales || !act_q || !act_scale || !out) return QIFT_ERR_NULL;
   if (dtype != QIFT_F16 && dtype != QIFT_BF16 && dtype != QIFT_F32) return QIFT_ERR_FORMAT;
   if (!shape_ok(w->N, w->K, M)) return QIFT_ERR_SHAPE;
-  const size_t need = qift::route::w8_workspace(w->N, M, w->K);
-  if (workspace_bytes > 0 && (!workspace || workspace_bytes < need)) return QIFT_ERR_WORKSPACE;
+  const qift::route::W8Plan plan = qift::route::w8_plan(w->N, M, w->K, workspace_bytes > 0);
+  if (workspace_bytes > 0 && (!workspace || workspace_bytes < qift::route::w8_workspace(plan, w->N, M))) return QIFT_ERR_WORKSPACE;
   const void* p[] = {w->levels, w->scales, act_q, act_scale, out, acc_out, workspace};
   for (const void* x : p)
     if (!aligned16(x)) return QIFT_ERR_ALIGN;
   const qift::W8Call c = {w->levels, w->scales, w->N, w->K, act_q, act_scale, M, out, acc_out,
                           workspace_bytes > 0 ? workspace : nullptr, dtype};
   const hipStream_t s = (hipStream_t)stream;
-  if (M <= qift::route::kW8RowsMaxM) return qift::report_hip(qift::launch_w8_rows(c, s));
-  qift::route::W8Plan plan = qift::route::w8_plan(w->N, M, w->K);
-  if (!c.ws) plan.parts = 1;
-  return qift::report_hip(qift::launch_w8_gemm(c, plan, s));
+  return qift::report_hip(plan.rows ? qift::launch_w8_rows(c, plan, s) : qift::launch_w8_gemm(c, plan, s));
 }
 
 }  // extern "C"

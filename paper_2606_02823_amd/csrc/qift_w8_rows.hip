@@ -1,10 +1,12 @@
-// The 8-bit linear for up to 64 tokens: one pass over the weights, K cut into a slice for each wave.
+// The 8-bit linear for up to 32 tokens: one pass over the weights, K cut into a slice for each wave.
 #include "qift_w8.h"
 
 namespace qift {
 namespace {
 
 using namespace w8;
+
+constexpr int kGroup = 8;
 
 // A workgroup owns 16 RT weight rows and all the tokens (TT tiles of 16).  Its waves take units of 64 U values of k in turn
 // (unit u is wave u mod NWV's), so that together they read whole pieces of each row; weights and codes go straight to the
@@ -15,7 +17,8 @@ template <int RT, int TT, int U, int NWV, int OT>
 __global__ __launch_bounds__(64 * NWV) void k_w8_rows(const int8_t* __restrict__ W, const uint16_t* __restrict__ sw, int64_t N,
                                                       int K, const int8_t* __restrict__ act, const float* __restrict__ sx,
                                                       int M, void* __restrict__ y, int32_t* __restrict__ acc_out) {
-  __shared__ __align__(16) v4i part[NWV][RT * TT][64];
+  constexpr int TG = RT * TT < kGroup ? RT * TT : kGroup;   // tiles whose sums meet at a time
+  __shared__ __align__(16) v4i part[NWV][TG][64];
   const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t n_base = (int64_t)blockIdx.x * (16 * RT);
@@ -67,22 +70,25 @@ __global__ __launch_bounds__(64 * NWV) void k_w8_rows(const int8_t* __restrict__
     use(u1);
   }
 #pragma unroll
-  for (int j = 0; j < RT; ++j)
+  for (int p0 = 0; p0 < RT * TT; p0 += TG) {
+    if (p0 > 0) __syncthreads();
 #pragma unroll
-    for (int t = 0; t < TT; ++t) part[wave][j * TT + t][lane] = acc[j][t];
-  __syncthreads();
-  for (int p = wave; p < RT * TT; p += NWV) {
-    v4i d = part[0][p][lane];
+    for (int i = 0; i < TG; ++i)
+      if (p0 + i < RT * TT) part[wave][i][lane] = acc[(p0 + i) / TT][(p0 + i) % TT];
+    __syncthreads();
+    for (int i = wave; i < TG && p0 + i < RT * TT; i += NWV) {
+      v4i d = part[0][i][lane];
 #pragma unroll
-    for (int w = 1; w < NWV; ++w) d += part[w][p][lane];
-    const int j = p / TT, t = p - j * TT, m = 16 * t + r;
-    const int64_t n0 = n_base + 16 * j + 4 * g;
-    if (m >= M || n0 >= N) continue;
-    const int a[4] = {d[0], d[1], d[2], d[3]};
-    float s4[4];
-    scales4(load_scales(sw, n0, N), s4);
-    store_quad<OT>(y, m, n0, N, quad<OT>(a, sx[m], s4));
-    if (acc_out) store_quad<kAcc>(acc_out, m, n0, N, quad<kAcc>(a, 0.f, s4));
+      for (int w = 1; w < NWV; ++w) d += part[w][i][lane];
+      const int j = (p0 + i) / TT, t = (p0 + i) - j * TT, m = 16 * t + r;
+      const int64_t n0 = n_base + 16 * j + 4 * g;
+      if (m >= M || n0 >= N) continue;
+      const int a[4] = {d[0], d[1], d[2], d[3]};
+      float s4[4];
+      scales4(load_scales(sw, n0, N), s4);
+      store_quad<OT>(y, m, n0, N, quad<OT>(a, sx[m], s4));
+      if (acc_out) store_quad<kAcc>(acc_out, m, n0, N, quad<kAcc>(a, 0.f, s4));
+    }
   }
 }
 
@@ -99,14 +105,14 @@ hipError_t launch_rows(const W8Call& c, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_w8_rows(const W8Call& c, hipStream_t s) {
-  const int tt = (int)((c.M + 15) / 16);
-  // 16 rows to a workgroup while that gives fewer than two workgroups to a CU, else 32, with more tokens 64
-  const int64_t tiles = (c.N + 15) / 16;
-  if (tt == 1) return tiles <= 512 ? launch_rows<1, 1, 4, 8>(c, s) : launch_rows<2, 1, 4, 8>(c, s);
-  if (tt == 2) return tiles <= 512 ? launch_rows<1, 2, 4, 8>(c, s) : tiles <= 1024 ? launch_rows<2, 2, 2, 8>(c, s) : launch_rows<4, 2, 2, 4>(c, s);
-  if (tt == 3) return tiles <= 512 ? launch_rows<1, 3, 2, 8>(c, s) : tiles <= 1024 ? launch_rows<2, 3, 2, 8>(c, s) : launch_rows<4, 3, 2, 4>(c, s);
-  return tiles <= 512 ? launch_rows<1, 4, 2, 8>(c, s) : tiles <= 1024 ? launch_rows<2, 4, 2, 8>(c, s) : launch_rows<4, 4, 2, 4>(c, s);
+hipError_t launch_w8_rows(const W8Call& c, const route::W8Plan& p, hipStream_t s) {
+  // longer units where a wave has few (4096 x 14336 at one token 13.5 us against 15.4), shorter ones where many workgroups
+  // share a CU (28672 x 4096 24.1 against 26.7)
+  if (c.M <= 16) {
+    if (p.rows == 32) return launch_rows<2, 1, 4, 4>(c, s);
+    return c.N <= 16 * 512 ? launch_rows<1, 1, 4, 8>(c, s) : launch_rows<1, 1, 2, 8>(c, s);
+  }
+  return p.rows == 16 ? launch_rows<1, 2, 2, 8>(c, s) : p.rows == 32 ? launch_rows<2, 2, 2, 4>(c, s) : launch_rows<4, 2, 2, 4>(c, s);
 }
 
 }  // namespace qift

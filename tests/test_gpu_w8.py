@@ -118,10 +118,11 @@ def test_linear_up_to_64_tokens(Q, M, N, K):
     L, q, s_w, s_x = operands(rng, N, K, M)
     acc = olin.int_dot(L, q)
     w, act = Q.W8(dev(L), dev(s_w)), Q.QAct(dev(q), dev(s_x))
-    assert Q.w8a8_workspace(w, M) is None
+    ws = Q.w8a8_workspace(w, M)
     for dt in OUT:
         got_acc = torch.full((M, N), -7, dtype=torch.int32, device="cuda")
         assert same(Q.w8a8_linear(w, act, dtype=dt, acc_out=got_acc), expect(acc, s_x, s_w, dt)), dt
+        assert same(Q.w8a8_linear(w, act, dtype=dt, workspace=ws), expect(acc, s_x, s_w, dt)), dt
         assert np.array_equal(got_acc.cpu().numpy(), acc)
 
 

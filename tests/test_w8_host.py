@@ -88,7 +88,7 @@ def test_linear_refuses(L):
 def test_workspace_query_of_unsupported_shapes(L):
     q = lambda N, K, M: L.qift_w8a8_workspace_bytes(ctypes.byref(qift.W8C(N, K, A, A)), M)  # noqa: E731
     assert q(0, 256, 100) == q(512, 100, 100) == q(512, 256, 0) == q(512, 1 << 20, 100) == 0
-    assert q(4096, 4096, 64) == 0
+    assert q(4096, 4096, 1) == 0
     assert L.qift_w8a8_workspace_bytes(None, 4) == 0
 
 
@@ -99,8 +99,8 @@ using namespace qift::route;
 int main() {
   long N, M, K;
   while (std::scanf("%ld %ld %ld", &N, &M, &K) == 3) {
-    const W8Plan p = w8_plan(N, M, K);
-    std::printf("%d %d %zu\\n", p.tile, p.parts, w8_workspace(N, M, K));
+    const W8Plan p = w8_plan(N, M, K, true), u = w8_plan(N, M, K, false);
+    std::printf("%d %d %d %d %zu %d %d\\n", p.rows, p.bn, p.bm, p.parts, w8_workspace(p, N, M), u.parts, u.rows ? u.rows : u.bm);
   }
 }
 """
@@ -111,20 +111,22 @@ def test_plan_limits(tmp_path):
     cxx = shutil.which("g++") or shutil.which("clang++") or "/opt/rocm/llvm/bin/clang++"
     (tmp_path / "probe.cpp").write_text(PROBE)
     subprocess.run([cxx, "-std=c++17", "-I", CSRC, str(tmp_path / "probe.cpp"), "-o", str(tmp_path / "probe")], check=True)
-    sizes = [(N, M, K) for N in (1, 63, 64, 129, 1024, 4096, 4099, 28672, 131072) for M in (1, 64, 65, 128, 333, 1024, 4096, 70000)
+    sizes = [(N, M, K) for N in (1, 63, 64, 129, 1024, 4096, 4099, 28672, 131072) for M in (1, 17, 24, 64, 65, 128, 333, 1024, 4096, 70000)
              for K in (64, 128, 256, 1088, 4096, 14336, 131072)]
     out = subprocess.run([str(tmp_path / "probe")], input="".join("%d %d %d\n" % s for s in sizes), text=True,
                          capture_output=True, check=True).stdout.splitlines()
-    split = 0
+    seen = set()
     for (N, M, K), line in zip(sizes, out):
-        tile, parts, ws = (int(v) for v in line.split())
-        assert tile in (128, 256) and 1 <= parts <= (K + 127) // 128
-        if M <= 64 or parts == 1:
-            assert ws == 0
+        rows, bn, bm, parts, ws, unsplit, kind = (int(v) for v in line.split())
+        assert unsplit == 1 and kind > 0
+        assert 1 <= parts <= (K + 127) // 128
+        if rows:
+            assert rows in (16, 32, 64) and M <= 32 and parts == 1
         else:
-            split += 1
-            assert ws == parts * M * ((N + 3) // 4 * 4) * 4 and M <= 65535
-    assert split > 10
+            assert (bn, bm) in ((128, 32), (128, 64), (128, 128), (256, 256)) and (bm > 32 or M <= 32)
+        assert ws == (0 if parts == 1 else parts * M * ((N + 3) // 4 * 4) * 4) and (parts == 1 or M <= 65535)
+        seen.add((rows, bm, parts > 1))
+    assert {(16, 0, False), (32, 0, False), (0, 32, False), (0, 64, True), (0, 128, False), (0, 256, False)} <= seen
 
 
 def test_oracle_codes_are_the_rationals():
