@@ -13,52 +13,48 @@ namespace qift {
 namespace {
 
 using step::kSeqs;
+constexpr int kAhead = 8;   // sequences of a thread whose numbers are read at once
 
 struct Sums {
   int64_t a, b;
 };
 
-// Sums over the workgroup's 256 threads.
-__device__ __forceinline__ Sums group_sums(Sums v, Sums* part) {
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) {
-    v.a += __shfl_xor((long long)v.a, d);
-    v.b += __shfl_xor((long long)v.b, d);
-  }
-  const int w = threadIdx.x >> 6;
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) part[w] = v;
-  __syncthreads();
-  return {part[0].a + part[1].a + part[2].a + part[3].a, part[0].b + part[1].b + part[2].b + part[3].b};
-}
-
-// Sums over the threads before this one; all: over the workgroup.
-__device__ __forceinline__ Sums sums_before(Sums v, Sums* part, Sums& all) {
+// Sums of v over the threads before this one and, in all, over the workgroup's 256; and of `other` over the workgroup.  One
+// barrier and one more before the next use of `part`.
+struct Scan {
+  Sums before, all, other;
+};
+__device__ __forceinline__ Scan scan(Sums v, Sums other, Sums (*part)[2]) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   Sums s = v;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
     const int64_t a = __shfl_up((long long)s.a, d), b = __shfl_up((long long)s.b, d);
+    other.a += __shfl_xor((long long)other.a, d);
+    other.b += __shfl_xor((long long)other.b, d);
     if (lane >= d) {
       s.a += a;
       s.b += b;
     }
   }
+  if (lane == 63) {
+    part[w][0] = s;
+    part[w][1] = other;
+  }
   __syncthreads();
-  if (lane == 63) part[w] = s;
-  __syncthreads();
-  all = {0, 0};
-  Sums before = {s.a - v.a, s.b - v.b};
+  Scan r = {{s.a - v.a, s.b - v.b}, {0, 0}, {0, 0}};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     if (i < w) {
-      before.a += part[i].a;
-      before.b += part[i].b;
+      r.before.a += part[i][0].a;
+      r.before.b += part[i][0].b;
     }
-    all.a += part[i].a;
-    all.b += part[i].b;
+    r.all.a += part[i][0].a;
+    r.all.b += part[i][0].b;
+    r.other.a += part[i][1].a;
+    r.other.b += part[i][1].b;
   }
-  return before;
+  return r;
 }
 
 __device__ __forceinline__ int64_t depth_of(const int32_t* count, int64_t capacity, bool& bad) {
@@ -67,31 +63,46 @@ __device__ __forceinline__ int64_t depth_of(const int32_t* count, int64_t capaci
   return c < 0 ? 0 : c > capacity ? capacity : c;
 }
 
+// (a sequence past the last before this workgroup's reads that one again, so that no load waits behind a branch)
+__device__ __forceinline__ int before_at(int b, int first) { return b < first ? b : first - 1; }
+
 // Bound by latency: the lengths, the table's or the stack's entry, the slot.
 __global__ __launch_bounds__(kSeqs) void k_plan(PlanCall c, pages::Div page, int split, uint32_t* err) {
-  __shared__ Sums part[4];
+  __shared__ Sums part[4][2];
   __shared__ int32_t s_start[kSeqs + 1], s_base[kSeqs + 1];   // from the workgroup's first sequence on
   __shared__ int32_t s_len[kSeqs], s_held[kSeqs], s_served[kSeqs];
   const int t = threadIdx.x;
   const int chunk = blockIdx.x / split, sub = blockIdx.x - chunk * split;
-  const int64_t first = (int64_t)chunk * kSeqs, room = (int64_t)c.table_pages * page.d;
+  const int first = chunk * kSeqs;   // (at most 65535 sequences)
+  const int64_t room = (int64_t)c.table_pages * page.d;
   const bool last = first + kSeqs >= c.B;
   bool bad;
+  const int64_t b = first + t;
+  const int32_t my_len = b < c.B ? c.lens[b] : 0, my_n = b < c.B ? c.counts[b] : 0;
   const int64_t depth = depth_of(c.free_count, c.capacity, bad);
   // the sequences before this workgroup's
   Sums before = {0, 0};
-  for (int64_t b = t; b < first; b += kSeqs) {
-    const step::Ask a = step::ask(c.lens[b], c.counts[b], room, page);
-    before.a += a.n;
-    before.b += a.need;
+  for (int b0 = 0; b0 < first; b0 += kAhead * kSeqs) {
+    int32_t len[kAhead], n[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int at = before_at(b0 + i * kSeqs + t, first);
+      len[i] = c.lens[at];
+      n[i] = c.counts[at];
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const step::Ask a = step::ask(len[i], n[i], room, page);
+      const bool in = b0 + i * kSeqs + t < first;
+      before.a += in ? a.n : 0;
+      before.b += in ? a.need : 0;
+    }
   }
-  if (chunk > 0) before = group_sums(before, part);
   // its own
-  const int64_t b = first + t;
-  step::Ask a = {0, 0, 0, 0, true, false};
-  if (b < c.B) a = step::ask(c.lens[b], c.counts[b], room, page);
-  Sums all;
-  const Sums own = sums_before({a.n, a.need}, part, all);
+  const step::Ask a = step::ask(my_len, my_n, room, page);
+  const Scan sums = scan({a.n, a.need}, before, part);
+  const Sums own = sums.before, all = sums.all;
+  before = sums.other;
   const int64_t start = before.a + own.a, base = before.b + own.b;
   const bool served = step::served(a, start, base, c.rows, depth);
   // (sums past every row and every page are cut: nothing behind them is served)
@@ -121,8 +132,8 @@ __global__ __launch_bounds__(kSeqs) void k_plan(PlanCall c, pages::Div page, int
       for (int64_t at = 0; at < c.B; at += kSeqs) {
         step::Ask o = {0, 0, 0, 0, true, false};
         if (at + t < c.B) o = step::ask(c.lens[at + t], c.counts[at + t], room, page);
-        Sums sum;
-        const Sums mine = sums_before({o.n, o.need}, part, sum);
+        const Scan round = scan({o.n, o.need}, {0, 0}, part);
+        const Sums mine = round.before, sum = round.all;
         const int64_t end = run.b + mine.b + o.need;
         int64_t most = step::served(o, run.a + mine.a, run.b + mine.b, c.rows, depth) ? end : 0;
 #pragma unroll
@@ -131,10 +142,11 @@ __global__ __launch_bounds__(kSeqs) void k_plan(PlanCall c, pages::Div page, int
           most = other > most ? other : most;
         }
         __syncthreads();
-        if ((t & 63) == 0) part[t >> 6].a = most;
+        if ((t & 63) == 0) part[t >> 6][0].a = most;
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) taken = part[i].a > taken ? part[i].a : taken;
+        for (int i = 0; i < 4; ++i) taken = part[i][0].a > taken ? part[i][0].a : taken;
+        __syncthreads();
         run.a += sum.a;
         run.b += sum.b;
       }
@@ -153,7 +165,7 @@ __global__ __launch_bounds__(kSeqs) void k_plan(PlanCall c, pages::Div page, int
       if (s_served[s]) {
         pos = s_len[s] + (int32_t)(r - s_start[s]);
         const uint32_t p = pages::quotient((uint32_t)pos, page);
-        const int32_t entry = (int32_t)p < s_held[s] ? c.table[(first + s) * c.table_pages + p]
+        const int32_t entry = (int32_t)p < s_held[s] ? c.table[(int64_t)(first + s) * c.table_pages + p]
                                                      : c.free_pages[depth - 1 - (before.b + s_base[s] + ((int32_t)p - s_held[s]))];
         slot = step::slot_of(entry, (uint32_t)pos - p * page.d, page.d);
         bad |= slot < 0;
@@ -168,33 +180,41 @@ __global__ __launch_bounds__(kSeqs) void k_plan(PlanCall c, pages::Div page, int
     const int s = step::find(s_base, kSeqs, (int32_t)f);
     if (!s_served[s]) continue;
     const int32_t entry = c.free_pages[depth - 1 - (before.b + f)];
-    c.table[(first + s) * c.table_pages + s_held[s] + (f - s_base[s])] = entry;
+    c.table[(int64_t)(first + s) * c.table_pages + s_held[s] + (f - s_base[s])] = entry;
     bad |= entry < 0;
   }
   if (bad) dev::flag_error(err, kDevErrIndex);
 }
 
 __global__ __launch_bounds__(kSeqs) void k_release(ReleaseCall c, pages::Div page, int split, uint32_t* err) {
-  __shared__ Sums part[4];
+  __shared__ Sums part[4][2];
   __shared__ int32_t s_base[kSeqs + 1];
   const int t = threadIdx.x;
   const int chunk = blockIdx.x / split, sub = blockIdx.x - chunk * split;
-  const int64_t first = (int64_t)chunk * kSeqs, room = (int64_t)c.table_pages * page.d;
+  const int first = chunk * kSeqs;   // (at most 65535 sequences)
+  const int64_t room = (int64_t)c.table_pages * page.d;
   const bool last = first + kSeqs >= c.B;
   bool bad;
+  const int64_t b = first + t;
+  const int32_t my_len = b < c.B ? c.lens[b] : 0;
+  const bool done = b < c.B && c.done[b] != 0;
   const int64_t depth = depth_of(c.free_count, c.capacity, bad);
   Sums before = {0, 0};
-  for (int64_t b = t; b < first; b += kSeqs) before.a += c.done[b] ? step::ask(c.lens[b], 0, room, page).held : 0;
-  if (chunk > 0) before = group_sums(before, part);
-  const int64_t b = first + t;
-  step::Ask a = {0, 0, 0, 0, true, false};
-  bool done = false;
-  if (b < c.B) {
-    a = step::ask(c.lens[b], 0, room, page);
-    done = c.done[b] != 0;
+  for (int b0 = 0; b0 < first; b0 += kAhead * kSeqs) {
+    int32_t len[kAhead], over[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int at = before_at(b0 + i * kSeqs + t, first);
+      len[i] = c.lens[at];
+      over[i] = c.done[at];
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) before.a += over[i] && b0 + i * kSeqs + t < first ? step::ask(len[i], 0, room, page).held : 0;
   }
-  Sums all;
-  const Sums own = sums_before({done ? a.held : 0, 0}, part, all);
+  const step::Ask a = step::ask(my_len, 0, room, page);
+  const Scan sums = scan({done ? a.held : 0, 0}, before, part);
+  const Sums own = sums.before, all = sums.all;
+  before = sums.other;
   auto cut = [](int64_t v) { return (int32_t)(v < 0x7FFFFFFF ? v : 0x7FFFFFFF); };
   s_base[t] = cut(own.a);
   if (t == 0) s_base[kSeqs] = cut(all.a);
@@ -210,17 +230,19 @@ __global__ __launch_bounds__(kSeqs) void k_release(ReleaseCall c, pages::Div pag
   for (int64_t f = (int64_t)sub * kSeqs + t; f < s_base[kSeqs]; f += (int64_t)split * kSeqs) {
     const int s = step::find(s_base, kSeqs, (int32_t)f);
     const int64_t at = depth + before.a + f;
-    const int32_t entry = c.table[(first + s) * c.table_pages + (f - s_base[s])];
+    const int32_t entry = c.table[(int64_t)(first + s) * c.table_pages + (f - s_base[s])];
     bad |= entry < 0 || at >= c.capacity;
     if (at < c.capacity) c.free_pages[at] = entry;
   }
   if (bad) dev::flag_error(err, kDevErrIndex);
 }
 
-// Parts of a workgroup's rows or pages, so that a part has about four to a thread, and no more workgroups than 4 to a CU
+// Parts of a workgroup's rows or pages, one to a thread, up to 8 workgroups to a CU: a row is a search and two reads, one behind
+// the other (2000 sequences with 116000 rows 7.8 us; 11.3
+// with four to a thread and the sequences before them read one by one)
 int splits(int64_t items, int64_t chunks) {
-  int64_t n = items / (chunks * 4 * kSeqs);
-  if (n > 1024 / chunks) n = 1024 / chunks;
+  int64_t n = (items + chunks * kSeqs - 1) / (chunks * kSeqs);
+  if (n > 2048 / chunks) n = 2048 / chunks;
   return n < 1 ? 1 : (int)n;
 }
 
