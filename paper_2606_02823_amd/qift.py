@@ -481,6 +481,14 @@ def _empty(shape, dtype, device, stream=None) -> torch.Tensor:
         return torch.empty(shape, dtype=dtype, device=device)
 
 
+def _empty_of(t, shape, stream=None) -> torch.Tensor:
+    """The same on t's device and of its type (0.5 us less than naming both)."""
+    if stream is None:
+        return t.new_empty(shape)
+    with torch.cuda.stream(stream):
+        return t.new_empty(shape)
+
+
 def _empty_pair(shape, dtype, device, stream=None):
     if stream is None:
         a = torch.empty(shape, dtype=dtype, device=device)
@@ -498,6 +506,10 @@ def _on_device(t, index, name, of="cache"):
         raise TypeError(f"{name} must be a CUDA (HIP) tensor")
     if t.get_device() != index:
         raise ValueError(f"{name} is on {t.device}, the {of} on device {index}")
+
+
+def _is(t, index, dtype, shape):
+    return t.__class__ is torch.Tensor and t.get_device() == index and t.dtype is dtype and t.shape == shape and t.is_contiguous()
 
 
 def _dense(t, index, dtype, shape, name, of="cache"):
@@ -624,7 +636,7 @@ def kv4_attention_tree(q: torch.Tensor, cache: KV4Pages, table: torch.Tensor, st
     return out
 
 
-@dataclass
+@dataclass(slots=True)
 class KV4Plan:
     """Where the new tokens of a step go (kv4_plan_step), all int32: starts [B + 1], lens [B] with the new tokens, slots and
     positions [rows], free_count [1] of the stack after the step.  lens and free_count are the next step's inputs."""
@@ -635,16 +647,22 @@ class KV4Plan:
     free_count: torch.Tensor
 
 
-def _step_tables(lens, table, free_pages, free_count):
+def _step_tables(lens, counts, table, free_pages, free_count, name):
     if table.dim() != 2 or free_pages.dim() != 1:
         raise ValueError(f"table must have shape (B, table_pages), free_pages (capacity,); got {tuple(table.shape)}, "
                          f"{tuple(free_pages.shape)}")
-    B, width = table.shape
+    B, width = shape = table.shape
     index = table.get_device()
-    _dense(table, index, torch.int32, (B, width), "table", "table")
-    _dense(lens, index, torch.int32, (B,), "lens", "table")
-    _dense(free_pages, index, torch.int32, free_pages.shape, "free_pages", "table")
-    _dense(free_count, index, torch.int32, (1,), "free_count", "table")
+    i32 = torch.int32
+    if not (_is(table, index, i32, shape) and index >= 0 and lens.shape == counts.shape == (B,)
+            and lens.dtype is counts.dtype is free_pages.dtype is free_count.dtype is i32 and free_count.shape == (1,)
+            and lens.get_device() == counts.get_device() == free_pages.get_device() == free_count.get_device() == index
+            and lens.is_contiguous() and counts.is_contiguous() and free_pages.is_contiguous()):
+        _dense(table, index, i32, shape, "table", "table")
+        _dense(lens, index, i32, (B,), "lens", "table")
+        _dense(counts, index, i32, (B,), name, "table")
+        _dense(free_pages, index, i32, free_pages.shape, "free_pages", "table")
+        _dense(free_count, index, i32, (1,), "free_count", "table")
     return B, width, index
 
 
@@ -654,10 +672,9 @@ def kv4_plan_step(lens: torch.Tensor, counts: torch.Tensor, table: torch.Tensor,
     ones (int32 [B]), their pages taken from the top of the stack free_pages[: free_count] (int32 [capacity], [1]) into
     table (int32 [B, table_pages], written in place).  rows: how many rows the step has room for.  What out names must be
     other tensors than lens and free_count."""
-    B, width, index = _step_tables(lens, table, free_pages, free_count)
-    _dense(counts, index, torch.int32, (B,), "counts", "table")
+    B, width, index = _step_tables(lens, counts, table, free_pages, free_count, "counts")
     if out is None:   # one piece of memory for the five
-        out = KV4Plan(*_empty((2 * B + 2 * rows + 2,), torch.int32, table.device, stream).split((B + 1, B, rows, rows, 1)))
+        out = KV4Plan(*_empty_of(table, 2 * B + 2 * rows + 2, stream).split_with_sizes((B + 1, B, rows, rows, 1)))
     else:
         _dense(out.starts, index, torch.int32, (B + 1,), "starts", "table")
         _dense(out.lens, index, torch.int32, (B,), "lens", "table")
@@ -677,10 +694,9 @@ def kv4_release(lens: torch.Tensor, done: torch.Tensor, table: torch.Tensor, fre
                 page: int, out=None, stream=None):
     """The pages of the sequences with done[b] != 0 (int32 [B]) put back on the stack (free_pages, written in place).
     Returns (lens, free_count) after that, new tensors or the pair out."""
-    B, width, index = _step_tables(lens, table, free_pages, free_count)
-    _dense(done, index, torch.int32, (B,), "done", "table")
+    B, width, index = _step_tables(lens, done, table, free_pages, free_count, "done")
     if out is None:
-        out = _empty((B + 1,), torch.int32, table.device, stream).split((B, 1))
+        out = _empty_of(table, B + 1, stream).split_with_sizes((B, 1))
     lens_out, free_out = out
     _dense(lens_out, index, torch.int32, (B,), "lens", "table")
     _dense(free_out, index, torch.int32, (1,), "free_count", "table")
@@ -733,7 +749,7 @@ def head_norm_rope(rope: HeadRope, q: torch.Tensor, k: torch.Tensor, positions: 
     ks = _rows(k, index, dt, (rows, Hkv, 128), "k", "frequencies")
     _dense(positions, index, torch.int32, (rows,), "positions", "frequencies")
     if out is None:
-        qo, ko = _empty((rows, Hq, 128), dt, q.device, stream), _empty((rows, Hkv, 128), dt, q.device, stream)
+        qo, ko = _empty_of(q, (rows, Hq, 128), stream), _empty_of(k, (rows, Hkv, 128), stream)
         qos, kos = Hq * 128, Hkv * 128
     else:
         qo, ko = out
