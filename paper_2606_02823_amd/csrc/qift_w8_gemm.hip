@@ -37,7 +37,7 @@ __device__ __forceinline__ int slot(int r, int c) { return c ^ (((r >> 1) & 7) ^
 // Both operands go to LDS without passing registers, NS - 1 steps ahead, in NS buffers that are distinct arrays (so that the
 // compiler sees that loads into one never alias reads from another, and adds no waits).  The barrier that hands a buffer over
 // stands before the last quarter of a step's products: by then the step's operands are in registers, so the loads of step
-// k + NS go out into its buffer, and the first operands of the next step are read behind the remaining products.
+// k + NS go out into its buffer, and the first operands of the next step are read between the remaining products.
 // Workgroup z of `parts` takes an even part of the steps; with more than one, the int32 sums go to `y` as [parts][M][N4].
 template <int TN, int TM, int GN, int GM, int NS, int OT>
 __global__ __launch_bounds__(64 * GN * GM) void k_w8_gemm(const int8_t* __restrict__ W, const uint16_t* __restrict__ sw, int64_t N,
@@ -142,19 +142,16 @@ __global__ __launch_bounds__(64 * GN * GM) void k_w8_gemm(const int8_t* __restri
     });
   };
   constexpr int AHEAD = (NS - 2) * (NA + NB);   // loads of later steps, in flight where a step hands its buffer over
-  constexpr int BEFORE = NP > 4 ? 2 : NP > 1 ? 1 : 0;   // products of the last quarter before the hand-over
-  constexpr int FIRST = NP > 4 ? NL / 2 : NL;     // loads that go out with those behind it; the others with the next step's first quarter
+  constexpr int FIRST = NL / 2;   // loads that go out with the last quarter; the others with the next step's first
   // `last` is the buffer that the step before handed over
   auto step = [&](int8_t* cur, int8_t* nxt, int8_t* last, int kt) QIFT_INLINE {
     quarter(cur, Const<1>(), Const<0>(), Const<0>(), last, (kt - 1 + NS) * kBK, Const<FIRST>(), Const<NL>());
     quarter(cur, Const<2>(), Const<1>(), Const<0>(), last, 0, Const<0>(), Const<0>());
     quarter(cur, Const<3>(), Const<0>(), Const<0>(), last, 0, Const<0>(), Const<0>());
-    each<BEFORE>([&](auto i) QIFT_INLINE { product(Const<1>(), i); });
-    __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_waitcnt(waits::encode(AHEAD, true));   // the last operands are here, and the next step's tiles
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
-    quarter(nxt, Const<0>(), Const<1>(), Const<BEFORE>(), cur, (kt + NS) * kBK, Const<0>(), Const<FIRST>());
+    quarter(nxt, Const<0>(), Const<1>(), Const<0>(), cur, (kt + NS) * kBK, Const<0>(), Const<FIRST>());
   };
   // the tile's scales for the end (their loads go out before the tiles')
   static_assert(BN <= 64 * NW && BM <= 64 * NW, "a scale to a thread");
@@ -263,12 +260,21 @@ __global__ __launch_bounds__(256) void k_w8_sum(const int32_t* __restrict__ ws, 
   const int64_t n0 = 4 * ((int64_t)blockIdx.x * 256 + threadIdx.x), m = blockIdx.y;
   if (n0 >= N) return;
   int a[4] = {0, 0, 0, 0};
-  for (int z = 0; z < parts; ++z) {
-    const int4 v = *reinterpret_cast<const int4*>(ws + ((int64_t)z * M + m) * N4 + n0);
-    a[0] += v.x;
-    a[1] += v.y;
-    a[2] += v.z;
-    a[3] += v.w;
+  for (int z0 = 0; z0 < parts; z0 += 4) {   // four parts' loads at once (one past the last: the last again, not added)
+    int4 v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int z = z0 + i < parts ? z0 + i : parts - 1;
+      v[i] = *reinterpret_cast<const int4*>(ws + ((int64_t)z * M + m) * N4 + n0);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (z0 + i < parts) {
+        a[0] += v[i].x;
+        a[1] += v[i].y;
+        a[2] += v[i].z;
+        a[3] += v[i].w;
+      }
   }
   float s4[4];
   scales4(load_scales(sw, n0, N), s4);
