@@ -73,7 +73,7 @@ int qift_kv4_release(const int32_t *lens, const int32_t *done, int64_t B, const 
  *   pairs      0: value i is paired with value i + rot / 2; 1: value 2 i with value 2 i + 1.
  *   freq       fp32 [rot / 2], finite: the angle of pair i at position p is p * freq[i].
  *   q_weight, k_weight   [head_dim] in the type of the rows, nullable: without one those heads are not normed.
- *   eps        positive and finite.
+ *   eps        finite, at least 2^-80 (squares that fp32 cannot hold are then nothing beside it).
  */
 typedef struct {
   int32_t head_dim;            /* 128 */
@@ -96,7 +96,8 @@ typedef struct {
  *   dtype       QIFT_F16 or QIFT_BF16.
  *   positions   int32 [rows].  A negative position: the row is padding, its outputs are zeros.
  *   q_out, k_out   out: as q and k, with strides of their own; the input itself with the input's stride is taken (each
- *               value is read before it is written), any other overlap is not.
+ *               value is read before it is written), any other overlap is not: the same pointer with another stride, q_out
+ *               at k, k_out at q or both outputs at one place are QIFT_ERR_SHAPE.
  * 16-byte aligned, positions 4.  rows = 0 does nothing.  Limits: rows * ceil((Hq + Hkv) / 4) < 2^26.  One launch.
  */
 int qift_head_norm_rope(const qift_head_rope *rope, const void *q, int64_t q_stride, const void *k, int64_t k_stride,

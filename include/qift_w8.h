@@ -32,7 +32,7 @@ typedef struct {
  * each row of the fp32 W [N][spec.K] rotated in fp64, s_w = fp16(max|w| / 127), q = clip(rne(w / s_w), -127, 127)
  * against the stored scale; a row whose stored scale is 0 gets zeros.
  *   spec, limits as for qift_quantize_weights (K a multiple of 64, at most 16384; block a power of two, 2..4096,
- *   dividing K; flags 0; N * K < 2^31).
+ *   dividing K; flags 0; N * K < 2^31), and N < 2^24.
  *   levels, scales   out: the fields of a qift_w8.
  */
 int qift_quantize_weights8(const float *W, int64_t N, qift_hadamard_spec spec, int8_t *levels, uint16_t *scales,
@@ -46,7 +46,7 @@ int qift_quantize_weights8(const float *W, int64_t N, qift_hadamard_spec spec, i
  * QIFT_CLIP and QIFT_SPEC_BF16 as there (bf16 tokens by the reading of qift_rotate_quant_act_bf16).
  *   x          fp16 or bf16 [M][spec.K], finite.
  *   act_q      out: int8 [M][K], act_scale out: fp32 [M].
- * Limits: spec.K <= 32768, block 2..8192.
+ * Limits: M < 2^23, spec.K <= 32768, block 2..8192.
  */
 int qift_rotate_quant_act8(const uint16_t *x, int64_t M, qift_hadamard_spec spec, int8_t *act_q, float *act_scale,
                            qift_stream_t stream);

@@ -57,7 +57,7 @@ int qift_head_norm_rope(const qift_head_rope* rope, const void* q, int64_t q_str
   if (!rope) return QIFT_ERR_NULL;
   if (dtype != QIFT_F16 && dtype != QIFT_BF16) return QIFT_ERR_FORMAT;
   if (rope->head_dim != 128 || rope->rot < 0 || rope->rot > 128 || rope->rot % 8) return QIFT_ERR_SHAPE;
-  if ((rope->pairs != 0 && rope->pairs != 1) || !(rope->eps > 0.f) || !isfinite(rope->eps)) return QIFT_ERR_SPEC;
+  if ((rope->pairs != 0 && rope->pairs != 1) || !(rope->eps >= 0x1p-80f) || !isfinite(rope->eps)) return QIFT_ERR_SPEC;
   if (rows < 0 || Hq < 0 || Hkv < 0 || Hq > 65535 || Hkv > 65535 || Hq + Hkv < 1) return QIFT_ERR_SHAPE;
   const int64_t groups = (Hq + Hkv + 3) / 4;
   if (rows >= k31 || rows * groups >= (int64_t(1) << 26)) return QIFT_ERR_SHAPE;
@@ -71,6 +71,10 @@ int qift_head_norm_rope(const qift_head_rope* rope, const void* q, int64_t q_str
   if (!positions || (rope->rot > 0 && !rope->freq)) return QIFT_ERR_NULL;
   for (int i = 0; i < 4; ++i)
     if ((i < 2 ? Hq : Hkv) > 0 && !rowsp[i]) return QIFT_ERR_NULL;
+  // each value is read before it is written where an output is its input; other overlaps race
+  if (rows > 1 && ((Hq > 0 && q == q_out && q_stride != q_out_stride) || (Hkv > 0 && k == k_out && k_stride != k_out_stride)))
+    return QIFT_ERR_SHAPE;
+  if (Hq > 0 && Hkv > 0 && (q_out == k || k_out == q || q_out == k_out)) return QIFT_ERR_SHAPE;
   for (int i = 0; i < 4; ++i)
     if ((i < 2 ? Hq : Hkv) > 0 && (!aligned(rowsp[i], 16) || strides[i] % 8)) return QIFT_ERR_ALIGN;
   if (!aligned(positions, 4) || !aligned(rope->freq, 16) || !aligned(rope->q_weight, 16) || !aligned(rope->k_weight, 16))

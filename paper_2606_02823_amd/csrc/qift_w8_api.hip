@@ -6,6 +6,7 @@
 namespace {
 
 constexpr int64_t k31 = int64_t(1) << 31;
+constexpr int64_t kRows24 = int64_t(1) << 24, kTokens23 = int64_t(1) << 23;   // workgroups of 256 and of 512: fewer than 2^32 threads
 constexpr int64_t kMaxK = 131072;   // 127 * 127 * K, and 128 * 128 * K, stay below 2^31
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -33,7 +34,7 @@ extern "C" {
 int qift_quantize_weights8(const float* W, int64_t N, qift_hadamard_spec spec, int8_t* levels, uint16_t* scales,
                            qift_stream_t stream) {
   if (!W || !levels || !scales) return QIFT_ERR_NULL;
-  if (N < 1 || N >= k31 || spec.K < 64 || spec.K % 64 || spec.K > qift::kWquantMaxK || N * spec.K >= k31) return QIFT_ERR_SHAPE;
+  if (N < 1 || N >= kRows24 || spec.K < 64 || spec.K % 64 || spec.K > qift::kWquantMaxK || N * spec.K >= k31) return QIFT_ERR_SHAPE;
   if (!block_ok(spec.block, 4096, spec.K) || spec.flags != 0) return QIFT_ERR_SPEC;
   if (!aligned16(W) || !aligned16(levels) || !aligned16(scales)) return QIFT_ERR_ALIGN;
   return qift::report_hip(qift::launch_quantize_weights8(W, N, spec.K, spec.block, levels, scales, (hipStream_t)stream));
@@ -42,7 +43,7 @@ int qift_quantize_weights8(const float* W, int64_t N, qift_hadamard_spec spec, i
 int qift_rotate_quant_act8(const uint16_t* x, int64_t M, qift_hadamard_spec spec, int8_t* act_q, float* act_scale,
                            qift_stream_t stream) {
   if (!x || !act_q || !act_scale) return QIFT_ERR_NULL;
-  if (M < 1 || M >= k31 || spec.K < 64 || spec.K % 64 || spec.K > qift::kActMaxK) return QIFT_ERR_SHAPE;
+  if (M < 1 || M >= kTokens23 || spec.K < 64 || spec.K % 64 || spec.K > qift::kActMaxK) return QIFT_ERR_SHAPE;
   const bool bf16 = (spec.flags & QIFT_SPEC_BF16) != 0;
   int num, den;
   if (!block_ok(spec.block, 8192, spec.K) || !clip_ok(spec.flags & ~QIFT_SPEC_BF16, &num, &den)) return QIFT_ERR_SPEC;

@@ -373,3 +373,81 @@ def test_a_step_of_a_layer(Q):
     assert Q.device_error() == 0
     held = [int(e) for b in (0, 2) for e in table.cpu()[b, :-(-int(lens[b]) // page)]]
     assert int(lens[1]) == 0 and sorted(held + free.cpu()[:int(depth)].tolist()) == list(range(pages))
+
+
+def test_a_captured_decode_step(Q):
+    """A decode step of 8-bit projection, plan, norms and rotation, append and attention in one graph, replayed over growing
+    sequences with eager steps between: every replay gives what the eager step on a copy of the same state gives."""
+    rng = np.random.default_rng(33)
+    B, Hq, Hkv, K, page, width, pages = 5, 8, 2, 512, 16, 4, 24
+    N = (Hq + 2 * Hkv) * 128
+    w = Q.quantize_weights8(dev(rng.normal(0, 0.05, (N, K)), torch.float32), 512)
+    wq, wk = (torch.from_numpy(rng.normal(1, 0.2, 128)).half().cuda() for _ in range(2))
+    rope = Q.HeadRope(dev(frequencies(96), torch.float32), 96, True, wq, wk)
+    work = Q.kv4_attention_tree_workspace(B, Hq, Hkv, 1, width * page)
+    x, counts = torch.zeros((B, K), dtype=torch.float16, device="cuda"), dev(np.ones(B))
+    ws = Q.w8a8_workspace(w, B)
+
+    class State:
+        def __init__(self):
+            self.cache = Q.KV4Pages.empty(pages, page, Hkv)
+            self.lens, self.table = dev(np.zeros(B)), dev(np.full((B, width), -1))
+            self.free, self.depth = dev(np.arange(pages)), dev([pages])
+
+        def step(self):
+            act = Q.rotate_quant_act8(x, 512)
+            qkv = Q.linear(w, act, workspace=ws)
+            q, k, v = (t.unflatten(1, (-1, 128)) for t in qkv.split([Hq * 128, Hkv * 128, Hkv * 128], dim=1))
+            p = Q.kv4_plan_step(self.lens, counts, self.table, self.free, self.depth, page, B)
+            Q.head_norm_rope(rope, q, k, p.positions, out=(q, k))
+            Q.kv4_append(self.cache, k, v, p.slots)
+            out = Q.kv4_attention_tree(q, self.cache, self.table, p.starts, p.lens, max_nodes=1, max_len=width * page, workspace=work)
+            self.lens.copy_(p.lens)
+            self.depth.copy_(p.free_count)
+            return out
+
+    a, b = State(), State()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        State().step()
+    torch.cuda.current_stream().wait_stream(s)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = a.step()
+    for i in range(20):
+        x.copy_(torch.from_numpy(rng.normal(0, 1, (B, K))))
+        counts.copy_(dev(rng.integers(0, 2, B)))
+        g.replay()
+        want = b.step()
+        torch.cuda.synchronize()
+        rows = int(counts.sum())
+        assert torch.equal(out[:rows], want[:rows]) and torch.equal(a.lens, b.lens) and torch.equal(a.table, b.table)
+        assert torch.equal(a.cache.k.codes, b.cache.k.codes) and torch.equal(a.cache.v.scales, b.cache.v.scales)
+
+
+def test_other_streams(Q):
+    """Each call on a stream given to it, several at once on several streams, and on a stream that is current."""
+    rng = np.random.default_rng(5)
+    rope = Q.HeadRope(dev(frequencies(128), torch.float32))
+    streams, results = [torch.cuda.Stream() for _ in range(3)], []
+    cases = []
+    for _ in range(3):
+        q, k = heads_of(rng, 900, 8, torch.float16).cuda(), heads_of(rng, 900, 2, torch.float16).cuda()
+        srv = Server(rng, rng.integers(0, 50, 300), 6, 16, 900)
+        cases.append((q, k, dev(rng.integers(0, 1000, 900)), [dev(t) for t in (srv.lens, rng.integers(0, 4, 300), srv.table, srv.free)],
+                      dev([srv.depth])))
+    torch.cuda.synchronize()
+    for s, (q, k, pos, (lens, counts, table, free), depth) in zip(streams, cases):
+        y = Q.head_norm_rope(rope, q, k, pos, stream=s)
+        p = Q.kv4_plan_step(lens, counts, table, free, depth, 16, 1000, stream=s)
+        r = Q.kv4_release(p.lens, torch.zeros_like(counts), table, free, p.free_count, 16, stream=s)
+        results.append((y, p, r))
+    torch.cuda.synchronize()
+    for (y, p, r), (q, k, pos, (lens, counts, table, free), depth) in zip(results, cases):
+        y2 = Q.head_norm_rope(rope, q, k, pos)
+        assert torch.equal(y[0], y2[0]) and torch.equal(y[1], y2[1])
+        p2 = Q.kv4_plan_step(lens, counts, table, free, depth, 16, 1000)    # the pages taken are the same again
+        assert torch.equal(p.starts, p2.starts) and torch.equal(p.positions, p2.positions) and torch.equal(p.lens, p2.lens)
+        assert torch.equal(p.slots, p2.slots) and torch.equal(p.free_count, p2.free_count)
+        assert torch.equal(r[0], p.lens) and torch.equal(r[1], p.free_count)

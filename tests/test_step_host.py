@@ -11,6 +11,7 @@ import pytest
 
 from oracle import step as ostep
 from paper_2606_02823_amd import qift
+from test_kernel_resources import kernels
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 CSRC = os.path.join(ROOT, "paper_2606_02823_amd", "csrc")
@@ -149,8 +150,8 @@ def test_release_refusals(L):
 
 
 def test_rope_refusals(L):
-    def f(head=128, rot=128, pairs=0, eps=1e-5, freq=A, qw=None, kw=None, q=A, qs=4096, k=A, ks=1024, dt=0, pos=A, rows=3, Hq=32,
-          Hkv=8, qo=A, qos=4096, ko=A, kos=1024):
+    def f(head=128, rot=128, pairs=0, eps=1e-5, freq=A, qw=None, kw=None, q=A, qs=4096, k=B_, ks=1024, dt=0, pos=A, rows=3, Hq=32,
+          Hkv=8, qo=A, qos=4096, ko=B_, kos=1024):
         r = qift.HeadRopeC(head, rot, pairs, eps, freq, qw, kw)
         return L.qift_head_norm_rope(ctypes.byref(r), q, qs, k, ks, dt, pos, rows, Hq, Hkv, qo, qos, ko, kos, None)
 
@@ -158,16 +159,23 @@ def test_rope_refusals(L):
     assert f(dt=2) == f(dt=-1) == E_FORMAT
     for kw in ({"head": 64}, {"rot": -8}, {"rot": 12}, {"rot": 136}, {"rows": -1}, {"Hq": -1}, {"Hkv": -1}, {"Hq": 0, "Hkv": 0},
                {"Hq": 65536}, {"qs": 4088}, {"ks": 1016}, {"qos": 4088}, {"kos": 1016}, {"qs": 2 ** 31}, {"rows": 2 ** 26},
-               {"rows": 2 ** 23}):
+               {"rows": 2 ** 23}, {"qos": 4104}, {"kos": 2048}, {"qo": B_}, {"ko": A}, {"qo": 0x40000, "ko": 0x40000}):
         assert f(**kw) == E_SHAPE, kw
-    for kw in ({"pairs": 2}, {"pairs": -1}, {"eps": 0.0}, {"eps": -1e-5}, {"eps": float("inf")}, {"eps": float("nan")}):
+    for kw in ({"pairs": 2}, {"pairs": -1}, {"eps": 0.0}, {"eps": 2.0 ** -81}, {"eps": -1e-5}, {"eps": float("inf")}, {"eps": float("nan")}):
         assert f(**kw) == E_SPEC, kw
     for kw in ({"freq": None}, {"q": None}, {"k": None}, {"pos": None}, {"qo": None}, {"ko": None}):
         assert f(**kw) == E_NULL, kw
     for kw in ({"freq": MIS}, {"qw": MIS}, {"kw": MIS}, {"q": MIS}, {"k": MIS}, {"qo": MIS}, {"ko": MIS}, {"pos": 0x10002},
-               {"qs": 4100}, {"ks": 1028}, {"qos": 4100}, {"kos": 1028}):
+               {"qs": 4100, "qos": 4100}, {"ks": 1028, "kos": 1028}, {"qo": 0x40000, "qos": 4100}, {"ko": 0x40000, "kos": 1028}):
         assert f(**kw) == E_ALIGN, kw
     assert f(rows=0) == OK and f(rows=0, q=None, pos=None) == OK
+
+
+@pytest.mark.parametrize("name,count", [("k_plan", 1), ("k_release", 1), ("k_rope", 12)])
+def test_no_spills(name, count):
+    ks = {k: v for k, v in kernels(qift.LIB_PATH).items() if f"{len(name)}{name}" in k}
+    assert len(ks) == count
+    assert not {k for k, v in ks.items() if v[".vgpr_spill_count"] or v[".private_segment_fixed_size"]}
 
 
 def test_oracle_plan():

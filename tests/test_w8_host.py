@@ -12,6 +12,7 @@ import pytest
 
 from oracle import hadamard, quant, w8
 from paper_2606_02823_amd import qift
+from test_kernel_resources import kernels
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 CSRC = os.path.join(ROOT, "paper_2606_02823_amd", "csrc")
@@ -52,8 +53,8 @@ def test_quantizers_refuse(L):
         assert wq(**kw) == E_NULL
     for kw in ({"x": None}, {"q": None}, {"sc": None}):
         assert aq(**kw) == E_NULL
-    assert wq(N=0) == wq(K=16384 + 64) == wq(N=2 ** 23) == E_SHAPE
-    assert aq(M=0) == aq(M=2 ** 31) == E_SHAPE
+    assert wq(N=0) == wq(K=16384 + 64) == wq(N=2 ** 23) == wq(N=2 ** 24, K=64) == E_SHAPE
+    assert aq(M=0) == aq(M=2 ** 31) == aq(M=2 ** 23) == E_SHAPE
     assert wq(block=8192, K=8192) == E_SPEC and wq(flags=qift.SPEC_BF16) == E_SPEC
     for flags in (1 << 17, qift.clip_flags(0, 4), qift.clip_flags(5, 4), qift.clip_flags(4, 17), -1):
         assert aq(flags=flags) == E_SPEC
@@ -127,6 +128,15 @@ def test_plan_limits(tmp_path):
         assert ws == (0 if parts == 1 else parts * M * ((N + 3) // 4 * 4) * 4) and (parts == 1 or M <= 65535)
         seen.add((rows, bm, parts > 1))
     assert {(16, 0, False), (32, 0, False), (0, 32, False), (0, 64, True), (0, 128, False), (0, 256, False)} <= seen
+
+
+@pytest.mark.parametrize("name,count", [("k_w8_rows", 18), ("k_w8_gemm", 16), ("k_w8_sum", 3)])
+def test_no_spills(name, count):
+    ks = {k: v for k, v in kernels(qift.LIB_PATH).items() if f"{len(name)}{name}I" in k}
+    assert len(ks) == count
+    assert not {k for k, v in ks.items() if v[".vgpr_spill_count"] or v[".private_segment_fixed_size"]}
+    if name == "k_w8_gemm":   # 256 x 256 tiles: a workgroup to a CU; the others leave room for two
+        assert all(v[".group_segment_fixed_size"] <= (163840 if "ILi4E" in k else 81920) for k, v in ks.items())
 
 
 def test_oracle_codes_are_the_rationals():
