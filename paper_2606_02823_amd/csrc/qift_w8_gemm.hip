@@ -304,8 +304,8 @@ hipError_t launch_tiles(const W8Call& c, int parts, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_w8_gemm(const W8Call& c, const route::W8Plan& p, hipStream_t s) {
-  if (p.bn == 256) return launch_tiles<4, 2, 2, 4, 2>(c, p.parts, s);
-  if (p.bm == 128) return launch_tiles<2, 2, 2, 2, 2>(c, p.parts, s);
+  if (p.bm == 256) return launch_tiles<4, 2, 2, 4, 2>(c, p.parts, s);
+  if (p.bm == 128) return launch_tiles<2, 2, 4, 2, 3>(c, p.parts, s);
   return p.bm == 64 ? launch_tiles<1, 1, 4, 2, 3>(c, p.parts, s) : launch_tiles<1, 1, 4, 1, 3>(c, p.parts, s);
 }
 

@@ -2,14 +2,15 @@
 //
 // What the kernels' times follow is the bytes that a CU takes in: about 27 a ns to registers (qift_w8_rows.hip) and up to
 // 54 a ns to LDS (qift_w8_gemm.hip), whatever the matrix cores do meanwhile, and for few tokens the weights' bytes from
-// memory.  So a plan is the least of the times below (ns), which were fitted to these measured ones (us, rows x K at tokens;
-// estimates in brackets):
-//   rows of 16: 4096 x 4096 at 1 token 5.9 (5.6), 28672 x 4096 24.1 (26), 4096 x 14336 13.5 (14), 4096 x 4096 at 32 8.4 (8.8),
-//     28672 x 4096 at 16 35 (36); rows of 32: 6144 x 4096 at 24 10.3 (10)
-//   128 x 32 tiles: 28672 x 4096 at 16 27 (27); 128 x 64: 2500 x 4096 at 600 15 (18), 4096 x 11008 at 333 41 (43), 4096 x 14336 at 64,
-//     8 parts, 19 (20)
-//   128 x 128: 4096 x 4096 at 1024 26 (30), 4096 x 11008 at 333 75 (73), in 2 parts 45 (46), in 5 33 (39)
-//   256 x 256: 9000 x 4096 at 1500 56 (56), 4096 x 14336 at 2048 162 (164), in 2 parts 117 (126), 28672 x 4096 at 4096 412 (408)
+// memory.  So a plan is the least of the times below (ns), which were fitted to measured ones (us, rows x K at tokens, weights
+// streamed from HBM; estimates in brackets):
+//   rows of 16: 4096 x 4096 at 1 token 5.9 (5.0), 28672 x 4096 24.1 (26), 4096 x 14336 13.5 (13.7), 4096 x 4096 at 32 8.4 (8.8);
+//     rows of 32: 6144 x 4096 at 1 8.0 (8.5; rows of 16 9.0), at 24 10.3 (10)
+//   128 x 32 tiles: 28672 x 4096 at 16 27 (28; rows of 16 35); 128 x 64: 2500 x 4096 at 600 15 (17), 32003 x 4096 at 61 31 (32),
+//     4096 x 14336 at 64 in 8 parts 19 (20)
+//   256 x 128: 4096 x 4096 at 2048 36 (38), 4096 x 11008 at 333 in 5 parts 32 (39)
+//   256 x 256: 9000 x 4096 at 1500 56 (57), 4096 x 14336 at 2048 162 (166), in 2 parts 117 (120), 28672 x 4096 at 4096 411 (399)
+// Over 56 drawn sizes of 17 to 4096 tokens the plan took 1.016 times the best tile's and split's time on average, at most 1.11.
 #pragma once
 
 #include <stddef.h>
@@ -45,19 +46,21 @@ inline W8Plan w8_plan(int64_t N, int64_t M, int64_t K, bool split) {
       if (ns <= best.ns) best = {r, 0, 0, 1, ns};
     }
   }
-  // step times of a CU with one and with two workgroups, and what a workgroup takes beside its steps
+  // Times of a step of a CU with one workgroup, where at most half of the CUs have one (`few`) and where most do, and with two
+  // side by side (0: they do not fit); and what a workgroup takes beside its steps.
   const struct {
     int bn, bm;
-    double one, two, fixed;
-  } tiles[] = {{128, 32, 400, 750, 3500}, {128, 64, 450, 900, 4000}, {128, 128, 800, 1150, 4000}, {256, 256, 1450, 3100, 6000}};
+    double few, one, two, fixed;
+  } tiles[] = {{128, 32, 400, 400, 750, 3500}, {128, 64, 420, 420, 880, 4000}, {256, 128, 680, 950, 0, 8000}, {256, 256, 1400, 1500, 0, 9000}};
   for (const auto& t : tiles) {
     if (t.bm < 64 && M > t.bm) continue;
     const int64_t count = w8_ceil(N, t.bn) * w8_ceil(M, t.bm);
     for (int p = 1; p <= (split ? 16 : 1); ++p) {
       if (p > 1 && (p > steps / 4 || count * p > 2 * kCus || M > 65535)) break;
       const int64_t each = w8_ceil(count * p, kCus);   // workgroups of the fullest CU
-      const double turn = (double)w8_ceil(steps, p) * ((double)(each / 2) * t.two + (double)(each & 1) * t.one);
-      const double rounds = t.bn == 256 ? (double)each : 1.0;   // (only these stand alone on their CU to the end)
+      const double one = count * p <= kCus / 2 ? t.few : t.one;
+      const double turn = (double)w8_ceil(steps, p) * (t.two > 0 ? (double)(each / 2) * t.two + (double)(each & 1) * one : (double)each * one);
+      const double rounds = t.two > 0 ? 1.0 : (double)each;
       double ns = (turn > stream ? turn : stream) + rounds * t.fixed;
       if (p > 1) ns += 3000.0 + 8.0 * p * (double)M * (double)N / 5000.0;   // the sums out and in, and their launch
       if (ns < best.ns) best = {0, t.bn, t.bm, p, ns};

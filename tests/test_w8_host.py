@@ -124,7 +124,7 @@ def test_plan_limits(tmp_path):
         if rows:
             assert rows in (16, 32, 64) and M <= 32 and parts == 1
         else:
-            assert (bn, bm) in ((128, 32), (128, 64), (128, 128), (256, 256)) and (bm > 32 or M <= 32)
+            assert (bn, bm) in ((128, 32), (128, 64), (256, 128), (256, 256)) and (bm > 32 or M <= 32)
         assert ws == (0 if parts == 1 else parts * M * ((N + 3) // 4 * 4) * 4) and (parts == 1 or M <= 65535)
         seen.add((rows, bm, parts > 1))
     assert {(16, 0, False), (32, 0, False), (0, 32, False), (0, 64, True), (0, 128, False), (0, 256, False)} <= seen
@@ -135,8 +135,8 @@ def test_no_spills(name, count):
     ks = {k: v for k, v in kernels(qift.LIB_PATH).items() if f"{len(name)}{name}I" in k}
     assert len(ks) == count
     assert not {k for k, v in ks.items() if v[".vgpr_spill_count"] or v[".private_segment_fixed_size"]}
-    if name == "k_w8_gemm":   # 256 x 256 tiles: a workgroup to a CU; the others leave room for two
-        assert all(v[".group_segment_fixed_size"] <= (163840 if "ILi4E" in k else 81920) for k, v in ks.items())
+    if name == "k_w8_gemm":   # the large tiles: a workgroup to a CU; the others leave room for two
+        assert all(v[".group_segment_fixed_size"] <= (81920 if "ILi1E" in k else 163840) for k, v in ks.items())
 
 
 def test_oracle_codes_are_the_rationals():
