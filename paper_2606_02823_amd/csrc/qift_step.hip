@@ -66,7 +66,8 @@ __device__ __forceinline__ int64_t depth_of(const int32_t* count, int64_t capaci
 // (a sequence past the last before this workgroup's reads that one again, so that no load waits behind a branch)
 __device__ __forceinline__ int before_at(int b, int first) { return b < first ? b : first - 1; }
 
-// Bound by latency: the lengths, the table's or the stack's entry, the slot.
+// Bound by latency: the lengths, the scan, the search, the table's or the stack's entry, the slot (61 sequences 4.8 us, an
+// empty launch 2.3).
 __global__ __launch_bounds__(kSeqs) void k_plan(PlanCall c, pages::Div page, int split, uint32_t* err) {
   __shared__ Sums part[4][2];
   __shared__ int32_t s_start[kSeqs + 1], s_base[kSeqs + 1];   // from the workgroup's first sequence on

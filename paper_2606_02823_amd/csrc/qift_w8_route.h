@@ -7,9 +7,9 @@
 //   rows of 16: 4096 x 4096 at 1 token 5.9 (5.0), 28672 x 4096 24.1 (26), 4096 x 14336 13.5 (13.7), 4096 x 4096 at 32 8.4 (8.8);
 //     rows of 32: 6144 x 4096 at 1 8.0 (8.5; rows of 16 9.0), at 24 10.3 (10)
 //   128 x 32 tiles: 28672 x 4096 at 16 27 (28; rows of 16 35); 128 x 64: 2500 x 4096 at 600 15 (17), 32003 x 4096 at 61 31 (32),
-//     4096 x 14336 at 64 in 8 parts 19 (20)
+//     4096 x 14336 at 64 in 8 parts 19 (23)
 //   256 x 128: 4096 x 4096 at 2048 36 (38), 4096 x 11008 at 333 in 5 parts 32 (39)
-//   256 x 256: 9000 x 4096 at 1500 56 (57), 4096 x 14336 at 2048 162 (166), in 2 parts 117 (120), 28672 x 4096 at 4096 411 (399)
+//   256 x 256: 9000 x 4096 at 1500 56 (57), 4096 x 14336 at 2048 162 (166), in 2 parts 117 (123), 28672 x 4096 at 4096 411 (399)
 // Over 56 drawn sizes of 17 to 4096 tokens the plan took 1.016 times the best tile's and split's time on average, at most 1.11.
 #pragma once
 

@@ -12,7 +12,9 @@ constexpr int kGroup = 8;
 // (unit u is wave u mod NWV's), so that together they read whole pieces of each row; weights and codes go straight to the
 // operands of the 16 x 16 x 64 product (lane (r, g): row or token r, values 16 g .. 16 g + 15 of each 64), the next unit's
 // loads sent before the present one is used.  The waves' sums meet in LDS, each wave adding up and storing some of the tiles.
-// Bound by the weights' bytes.
+// Bound by the weights' bytes with few tokens (28672 x 4096 at one 24.1 us, 4.9 TB/s; 4096 x 14336 13.5, 4.4; 4096 x 4096 5.9,
+// of which 2.5 are the launch and the first loads), with more by what a CU takes into registers, about 27 bytes a ns
+// (4096 x 4096 at 32 tokens 8.4 us): tiled products (qift_w8_gemm.hip) take over there.
 template <int RT, int TT, int U, int NWV, int OT>
 __global__ __launch_bounds__(64 * NWV) void k_w8_rows(const int8_t* __restrict__ W, const uint16_t* __restrict__ sw, int64_t N,
                                                       int K, const int8_t* __restrict__ act, const float* __restrict__ sx,
