@@ -53,20 +53,28 @@ __device__ __forceinline__ Quad<OT> quad(const int (&a)[4], float s_x, const flo
 template <int OT>
 constexpr int size_of() { return OT == kF16 || OT == kBF16 ? 2 : 4; }
 
-// The quad of outputs n0 .. n0 + 3 of token m: at once where its place is aligned and all of it is there.
-template <int OT>
-__device__ __forceinline__ void store_quad(void* y, int64_t m, int64_t n0, int64_t N, const Quad<OT>& v) {
-  const int64_t at = m * N + n0;
-  if (n0 + 4 <= N && (N & 3) == 0) {
-    *reinterpret_cast<Quad<OT>*>(static_cast<uint8_t*>(y) + at * size_of<OT>()) = v;
+// Vectors at any multiple of two bytes: rows of y begin at m N, and the compiler stores such vectors whole on this target.
+typedef uint32_t words2 __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t words4 __attribute__((ext_vector_type(4), aligned(2)));
+__device__ __forceinline__ void store_words(uint8_t* to, const uint2& v) { *reinterpret_cast<words2*>(to) = words2{v.x, v.y}; }
+__device__ __forceinline__ void store_words(uint8_t* to, const uint4& v) {
+  *reinterpret_cast<words4*>(to) = words4{v.x, v.y, v.z, v.w};
+}
+// The outputs n0 .. of token m that v holds, those below N.
+template <int OT, typename V>
+__device__ __forceinline__ void store_row(void* y, int64_t m, int64_t n0, int64_t N, const V& v) {
+  constexpr int SZ = size_of<OT>(), E = sizeof(V) / SZ;
+  uint8_t* to = static_cast<uint8_t*>(y) + (m * N + n0) * SZ;
+  if (n0 + E <= N) {
+    store_words(to, v);
     return;
   }
   const uint32_t* w = reinterpret_cast<const uint32_t*>(&v);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < E; ++i) {
     if (n0 + i >= N) break;
-    if constexpr (size_of<OT>() == 2) static_cast<uint16_t*>(y)[at + i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
-    else static_cast<uint32_t*>(y)[at + i] = w[i];
+    if constexpr (SZ == 2) reinterpret_cast<uint16_t*>(to)[i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+    else reinterpret_cast<uint32_t*>(to)[i] = w[i];
   }
 }
 

@@ -201,15 +201,17 @@ __global__ __launch_bounds__(64 * GN * GM) void k_w8_gemm(const int8_t* __restri
 
   // D of tile (j, t): register 4 q + i of lane (token r32, half h) is row 32 j + 8 q + 4 h + i.  Through the wave's own part
   // of the idle buffers, a token tile at a time: rows of 32 TN outputs in chunks of 16 bytes, chunk c of token m in slot
-  // c ^ m, then whole pieces of the rows of y.
+  // c ^ m, then 16-byte pieces of the rows of y, which begin at any place where N is no multiple of 8 (28671 x 4096 at 4096 tokens
+  // 424 us; value by value 460).
   constexpr int SZ = size_of<OT>(), ROW = 32 * TN * SZ, CH = ROW / 16;
   constexpr int PER = (BN + BM) * kBK / (32 * ROW);   // waves whose rows one of the buffers holds
   static_assert(PER * NS >= NW, "the waves' rows fit the buffers");
   int8_t* const mine = (wave < PER ? lds0 : wave < 2 * PER ? lds1 : wave < 3 * PER ? lds2 : lds3) + wave % PER * (32 * ROW);
   const int64_t n_wave = n_base + 32 * TN * wn;
   const int64_t NY = OT == kAcc ? (N + 3) & ~int64_t(3) : N;
+  constexpr int E = 16 / SZ;
+  const int have = NY - n_wave > 32 * TN ? 32 * TN : NY > n_wave ? (int)(NY - n_wave) : 0, last = have / E * E, rest = have - last;
   uint8_t* out = static_cast<uint8_t*>(y) + (OT == kAcc ? (int64_t)z * M * NY * 4 : 0);
-  const bool whole = NY % (16 / SZ) == 0;
 #pragma unroll
   for (int t = 0; t < TM; ++t) {
     const int64_t m0 = m_base + 32 * (TM * wm + t);
@@ -226,30 +228,26 @@ __global__ __launch_bounds__(64 * GN * GM) void k_w8_gemm(const int8_t* __restri
         const int at = n * SZ;
         *reinterpret_cast<Quad<OT>*>(mine + r32 * ROW + 16 * ((at >> 4) ^ (r32 & (CH - 1))) + (at & 15)) = quad<OT>(d, s_x, s4);
         if (OT != kAcc && acc_out && m0 + r32 < M && n_wave + n < N)
-          store_quad<kAcc>(acc_out, m0 + r32, n_wave + n, N, quad<kAcc>(d, 0.f, s4));
+          store_row<kAcc>(acc_out, m0 + r32, n_wave + n, N, quad<kAcc>(d, 0.f, s4));
       }
     __builtin_amdgcn_wave_barrier();
-    if (whole) {
-      constexpr int RI = 64 / CH;   // rows of one store
+    constexpr int RI = 64 / CH;   // rows of one store
 #pragma unroll
-      for (int i = 0; i < 32 / RI; ++i) {
-        const int rr = RI * i + lane / CH, c = lane % CH;
-        const uint4 v = *reinterpret_cast<const uint4*>(mine + rr * ROW + 16 * (c ^ (rr & (CH - 1))));
-        const int64_t m = m0 + rr, n = n_wave + c * (16 / SZ);
-        if (m < M && n < NY) *reinterpret_cast<uint4*>(out + (m * NY + n) * SZ) = v;
-      }
-    } else {
-#pragma unroll 4
-      for (int i = 0; i < 32 * TN * 32 / 64; ++i) {
-        const int rr = (64 * i) / (32 * TN) + (64 > 32 * TN ? lane / (32 * TN) : 0), n = (64 * i + lane) % (32 * TN);
-        const int at = n * SZ;
-        const int8_t* from = mine + rr * ROW + 16 * ((at >> 4) ^ (rr & (CH - 1))) + (at & 15);
-        const int64_t m = m0 + rr;
-        if (m < M && n_wave + n < N) {
-          if constexpr (SZ == 2)
-            *reinterpret_cast<uint16_t*>(out + (m * NY + n_wave + n) * 2) = *reinterpret_cast<const uint16_t*>(from);
-          else
-            *reinterpret_cast<uint32_t*>(out + (m * NY + n_wave + n) * 4) = *reinterpret_cast<const uint32_t*>(from);
+    for (int i = 0; i < 32 / RI; ++i) {
+      const int rr = RI * i + lane / CH, c = lane % CH;
+      const uint4 v = *reinterpret_cast<const uint4*>(mine + rr * ROW + 16 * (c ^ (rr & (CH - 1))));
+      const int64_t m = m0 + rr, n = n_wave + c * (16 / SZ);
+      if (m < M && n + E <= NY) store_words(out + (m * NY + n) * SZ, v);
+    }
+    if (rest > 0) {   // the values of the last row of weights' piece that do not fill 16 bytes
+#pragma unroll 1
+      for (int i = 0; i < 32 * E / 64; ++i) {
+        const int rr = (64 * i + lane) / E, n = last + (64 * i + lane) % E, place = n * SZ;
+        const int8_t* from = mine + rr * ROW + 16 * ((place >> 4) ^ (rr & (CH - 1))) + (place & 15);
+        if (m0 + rr < M && (64 * i + lane) % E < rest) {
+          uint8_t* to = out + ((m0 + rr) * NY + n_wave + n) * SZ;
+          if constexpr (SZ == 2) *reinterpret_cast<uint16_t*>(to) = *reinterpret_cast<const uint16_t*>(from);
+          else *reinterpret_cast<uint32_t*>(to) = *reinterpret_cast<const uint32_t*>(from);
         }
       }
     }
@@ -283,8 +281,8 @@ __global__ __launch_bounds__(256) void k_w8_sum(const int32_t* __restrict__ ws, 
   }
   float s4[4];
   scales4(load_scales(sw, n0, N), s4);
-  store_quad<OT>(y, m, n0, N, quad<OT>(a, sx[m], s4));
-  if (acc_out) store_quad<kAcc>(acc_out, m, n0, N, quad<kAcc>(a, 0.f, s4));
+  store_row<OT>(y, m, n0, N, quad<OT>(a, sx[m], s4));
+  if (acc_out) store_row<kAcc>(acc_out, m, n0, N, quad<kAcc>(a, 0.f, s4));
 }
 
 template <int TN, int TM, int GN, int GM, int NS>

@@ -88,8 +88,8 @@ __global__ __launch_bounds__(64 * NWV) void k_w8_rows(const int8_t* __restrict__
       const int a[4] = {d[0], d[1], d[2], d[3]};
       float s4[4];
       scales4(load_scales(sw, n0, N), s4);
-      store_quad<OT>(y, m, n0, N, quad<OT>(a, sx[m], s4));
-      if (acc_out) store_quad<kAcc>(acc_out, m, n0, N, quad<kAcc>(a, 0.f, s4));
+      store_row<OT>(y, m, n0, N, quad<OT>(a, sx[m], s4));
+      if (acc_out) store_row<kAcc>(acc_out, m, n0, N, quad<kAcc>(a, 0.f, s4));
     }
   }
 }
