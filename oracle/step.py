@@ -35,7 +35,7 @@ def plan(lens, counts, table, free, depth, page, rows):
                 slots[start + i] = slot if entry >= 0 and slot < 2 ** 31 else -1
                 bad |= slots[start + i] < 0
             lens_out[b] = have + n
-            taken = base + need
+            taken = base + need if need else taken
         else:
             bad |= n > 0
         start += n

@@ -31,10 +31,14 @@ QIFT_HD Ask ask(int32_t len, int32_t n, int64_t room, pages::Div page) {
   return a;
 }
 // Whether a sequence has its tokens in this step: start and base are the sums of the new tokens and of the pages that the
-// sequences before it ask for.  Both only grow, so of the sequences that need pages those served are the first ones, and
-// the pages taken are those up to the last one served.
+// sequences before it ask for.  Both only grow, so of the sequences that need pages those served are the first ones.
 QIFT_HD bool served(const Ask& a, int64_t start, int64_t base, int64_t rows, int64_t depth) {
   return a.n > 0 && a.fits && start + a.n <= rows && (a.need == 0 || base + a.need <= depth);
+}
+// The pages taken up to this sequence's last, where it takes any (one that needs none is served however many those before it
+// asked for in vain); a step takes the most of these.
+QIFT_HD int64_t taken(const Ask& a, int64_t start, int64_t base, int64_t rows, int64_t depth) {
+  return a.need > 0 && served(a, start, base, rows, depth) ? base + a.need : 0;
 }
 // Slot of the token at position pos whose page is `entry`; -1 where that is none or the slot has no 31 bits.
 QIFT_HD int32_t slot_of(int32_t entry, uint32_t at, uint32_t page) {

@@ -125,7 +125,7 @@ __global__ __launch_bounds__(kSeqs) void k_plan(PlanCall c, pages::Div page, int
   }
   __syncthreads();
   if (last && sub == 0) {
-    // the pages taken: all that are asked for, or, where something was left out, those up to the last sequence served
+    // the pages taken: all that are asked for, or, where something was left out, those up to the last sequence that takes some
     int64_t taken = before.b + all.b;
     if (taken > depth || before.a + all.a > c.rows) {
       taken = 0;
@@ -135,8 +135,7 @@ __global__ __launch_bounds__(kSeqs) void k_plan(PlanCall c, pages::Div page, int
         if (at + t < c.B) o = step::ask(c.lens[at + t], c.counts[at + t], room, page);
         const Scan round = scan({o.n, o.need}, {0, 0}, part);
         const Sums mine = round.before, sum = round.all;
-        const int64_t end = run.b + mine.b + o.need;
-        int64_t most = step::served(o, run.a + mine.a, run.b + mine.b, c.rows, depth) ? end : 0;
+        int64_t most = step::taken(o, run.a + mine.a, run.b + mine.b, c.rows, depth);
 #pragma unroll
         for (int d = 32; d > 0; d >>= 1) {
           const int64_t other = __shfl_xor((long long)most, d);

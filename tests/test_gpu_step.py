@@ -105,6 +105,20 @@ def test_plans_that_leave_sequences_out(Q, B):
             check_plan(Q, s, counts, rows, depth)
 
 
+def test_plans_where_pages_run_out(Q):
+    """Sequences that need no page behind ones that found too few: the stack keeps what nobody took."""
+    rng = np.random.default_rng(21)
+    s = Server(rng, [0, 1], 10, 16, 5)
+    want = check_plan(Q, s, np.array([160, 1]), 170)
+    assert want[5] == 5 and list(want[1]) == [0, 2]
+    for B in (7, 256, 600):
+        s = Server(rng, rng.integers(0, 60, B), 5, 16, 3 * B)
+        counts = rng.integers(0, 20, B)
+        for depth in (B // 2, 2, 0):
+            want = check_plan(Q, s, counts, int(counts.sum()), depth)
+            assert 0 <= want[5] <= depth and (want[6] or depth > 0)
+
+
 def test_plan_with_numbers_out_of_range(Q):
     rng = np.random.default_rng(7)
     width, page = 4, 32

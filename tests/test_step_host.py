@@ -33,6 +33,11 @@ int main() {
       std::scanf("%d %d %d %d", &len, &n, &width, &page);
       const step::Ask a = step::ask(len, n, (long long)width * page, pages::make_div((unsigned)page));
       std::printf("%d %d %d %d %d %d\n", a.len, a.n, a.held, a.need, (int)a.fits, (int)a.bad);
+    } else if (!std::strcmp(what, "taken")) {
+      int len, n, page, width, start, base, rows, depth;
+      std::scanf("%d %d %d %d %d %d %d %d", &len, &n, &width, &page, &start, &base, &rows, &depth);
+      const step::Ask a = step::ask(len, n, (long long)width * page, pages::make_div((unsigned)page));
+      std::printf("%d\n", (int)step::taken(a, start, base, rows, depth));
     } else if (!std::strcmp(what, "slot")) {
       int entry, at, page;
       std::scanf("%d %d %d", &entry, &at, &page);
@@ -197,6 +202,45 @@ def test_oracle_plan():
         done = (rng.random(B) < 0.2) | (lens > 60)
         lens, free, depth, bad = ostep.release(lens, done.astype(np.int32), table, free, depth, page)
         assert not bad
+
+
+def test_oracle_plan_where_pages_run_out():
+    """A sequence that needs no page takes none, whatever those before it asked for; no page is lost or had twice."""
+    table, free = np.array([[-1] * 10, [6] + [-1] * 9], np.int32), np.arange(5, dtype=np.int32)
+    got = ostep.plan(np.array([0, 1]), np.array([160, 1]), table, free, 5, 16, 170)
+    assert list(got[1]) == [0, 2] and got[3][160] == 97 and got[5] == 5 and got[6]
+    rng = np.random.default_rng(3)
+    B, width, page, pages, short = 8, 5, 16, 14, 0
+    lens, table, free, depth = np.zeros(B, np.int32), np.full((B, width), -1, np.int32), np.arange(pages, dtype=np.int32), pages
+    for _ in range(200):
+        counts = rng.integers(0, 20, B).astype(np.int32)
+        _, lens, table, _, _, depth, bad = ostep.plan(lens, counts, table, free, depth, page, 100)
+        short += bad
+        live = [int(p) for b in range(B) for p in table[b, :-(-int(lens[b]) // page)]]
+        assert sorted(live + [int(p) for p in free[:depth]]) == list(range(pages))
+        done = (rng.random(B) < 0.1) | (lens > 60)
+        lens, free, depth, bad = ostep.release(lens, done.astype(np.int32), table, free, depth, page)
+        assert not bad
+    assert 20 < short < 200
+
+
+def test_pages_taken_up_to_a_sequence(probe):
+    """The largest of these over the sequences is what the oracle takes."""
+    rng = np.random.default_rng(8)
+    lines, want, sizes = [], [], []
+    for _ in range(60):
+        B, width, page = int(rng.integers(1, 9)), 5, 16
+        lens, counts = rng.integers(0, 70, B), rng.integers(0, 30, B)
+        rows, depth = int(rng.integers(0, counts.sum() + 2)), int(rng.integers(0, 20))
+        start = base = 0
+        for n, c in zip(lens, counts):
+            lines.append(f"taken {n} {c} {width} {page} {start} {base} {rows} {depth}")
+            start += int(c)
+            base += -(-(n + c) // page) - -(-n // page) if n + c <= width * page else 0
+        sizes.append(B)
+        want.append(depth - ostep.plan(lens, counts, np.zeros((B, width), np.int32), np.zeros(depth, np.int32), depth, page, rows)[5])
+    got = iter(v for v, in probe(lines))
+    assert [max(next(got) for _ in range(n)) for n in sizes] == want
 
 
 def test_oracle_rotation():
