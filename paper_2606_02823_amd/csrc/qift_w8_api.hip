@@ -7,7 +7,7 @@ namespace {
 
 constexpr int64_t k31 = int64_t(1) << 31;
 constexpr int64_t kRows24 = int64_t(1) << 24, kTokens23 = int64_t(1) << 23;   // workgroups of 256 and of 512: fewer than 2^32 threads
-constexpr int64_t kMaxK = 131072;   // 127 * 127 * K, and 128 * 128 * K, stay below 2^31
+constexpr int64_t kMaxK = 131072;   // 127 * 127 * K stays below 2^31
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 

@@ -38,11 +38,11 @@ __device__ __forceinline__ int slot(int r, int c) { return c ^ (((r >> 1) & 7) ^
 // compiler sees that loads into one never alias reads from another, and adds no waits).  The barrier that hands a buffer over
 // stands before the last quarter of a step's products: by then the step's operands are in registers, so the loads of step
 // k + NS go out into its buffer, and the first operands of the next step are read between the remaining products.
-// What bounds the largest tiles is the chip's power: the matrix units are busy 68 % of the time at 1.56 GHz (28672 x 4096 at 4096
-// tokens, 411 to 445 us from card to card, 2.2 to 2.3 POP/s; the library's 8192 x 8192 x 8192 2.42 to 2.55, this one at 4096 tokens 2.53).  Of
-// the 411 us 50 go into storing the outputs, 54 are lost to the loads and 26 to the reads of LDS.  The smaller tiles are
-// bound by the bytes that a CU takes into LDS (2500 x 4096 at 600 tokens 15 us, 4096 x 11008 at 333 in five parts 32) or, with few
-// tokens, by the weights' bytes (32003 x 4096 at 61 tokens 31 us, 4.2 TB/s).
+// What bounds the largest tiles is the chip's power: the matrix units are busy 68 % of the time at 1.56 GHz (28672 x 4096 at
+// 4096 tokens, 411 to 445 us from card to card, 2.2 to 2.3 POP/s; the library's 8192 x 8192 x 8192 2.42 to 2.55, this one at 4096
+// tokens 2.53).  Of the 411 us 50 go into storing the outputs, 54 are lost to the loads and 26 to the reads of LDS.  The
+// smaller tiles are bound by the bytes that a CU takes into LDS (2500 x 4096 at 600 tokens 15 us, 4096 x 11008 at 333 in five
+// parts 32) or, with few tokens, by the weights' bytes (32003 x 4096 at 61 tokens 31 us, 4.2 TB/s).
 // Workgroup z of `parts` takes an even part of the steps; with more than one, the int32 sums go to `y` as [parts][M][N4].
 template <int TN, int TM, int GN, int GM, int NS, int OT>
 __global__ __launch_bounds__(64 * GN * GM) void k_w8_gemm(const int8_t* __restrict__ W, const uint16_t* __restrict__ sw, int64_t N,
@@ -52,11 +52,10 @@ __global__ __launch_bounds__(64 * GN * GM) void k_w8_gemm(const int8_t* __restri
   constexpr int NW = GN * GM, BN = 32 * TN * GN, BM = 32 * TM * GM;
   constexpr int NA = BN / (8 * NW), NB = BM / (8 * NW);   // direct-to-LDS loads of a wave and step, 8 rows each
   static_assert(NA * 8 * NW == BN && NB * 8 * NW == BM, "whole loads");
-  static_assert(NS >= 2 && NS <= 4 && (NS - 2) * (NA + NB) < 64, "buffers, and six bits of vmcnt");
+  static_assert((NS == 2 || NS == 3) && waits::w8_prologue(NS, NA + NB) < 64, "buffers, and six bits of vmcnt");
   __shared__ __align__(16) int8_t lds0[(BN + BM) * kBK];
   __shared__ __align__(16) int8_t lds1[(BN + BM) * kBK];
   __shared__ __align__(16) int8_t lds2[NS > 2 ? (BN + BM) * kBK : 16];
-  __shared__ __align__(16) int8_t lds3[NS > 3 ? (BN + BM) * kBK : 16];
   __shared__ __align__(16) float s_sx[BM];
   __shared__ __align__(16) uint16_t s_sw[BN];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -146,14 +145,13 @@ __global__ __launch_bounds__(64 * GN * GM) void k_w8_gemm(const int8_t* __restri
       __builtin_amdgcn_sched_barrier(0);
     });
   };
-  constexpr int AHEAD = (NS - 2) * (NA + NB);   // loads of later steps, in flight where a step hands its buffer over
-  constexpr int FIRST = NL / 2;   // loads that go out with the last quarter; the others with the next step's first
+  constexpr int FIRST = waits::w8_first(NL);   // loads that go out with the last quarter; the others with the next step's first
   // `last` is the buffer that the step before handed over
   auto step = [&](int8_t* cur, int8_t* nxt, int8_t* last, int kt) QIFT_INLINE {
     quarter(cur, Const<1>(), Const<0>(), Const<0>(), last, (kt - 1 + NS) * kBK, Const<FIRST>(), Const<NL>());
     quarter(cur, Const<2>(), Const<1>(), Const<0>(), last, 0, Const<0>(), Const<0>());
     quarter(cur, Const<3>(), Const<0>(), Const<0>(), last, 0, Const<0>(), Const<0>());
-    __builtin_amdgcn_s_waitcnt(waits::encode(AHEAD, true));   // the last operands are here, and the next step's tiles
+    __builtin_amdgcn_s_waitcnt(waits::encode(waits::w8_handover(NS, NL), true));   // the last operands, the next step's tiles
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
     quarter(nxt, Const<0>(), Const<1>(), Const<0>(), cur, (kt + NS) * kBK, Const<0>(), Const<FIRST>());
@@ -167,10 +165,9 @@ __global__ __launch_bounds__(64 * GN * GM) void k_w8_gemm(const int8_t* __restri
     if (tid < rows_n) sw_pre = sw[n_base + tid];
   }
   __builtin_amdgcn_sched_barrier(0);
-  int8_t* const lds_last = NS == 2 ? lds1 : NS == 3 ? lds2 : lds3;
+  int8_t* const lds_last = NS == 2 ? lds1 : lds2;
   each<NL>([&](auto i) QIFT_INLINE { issue(lds0, k_first * kBK, i); });
   if constexpr (NS > 2) each<NL>([&](auto i) QIFT_INLINE { issue(lds1, (k_first + 1) * kBK, i); });
-  if constexpr (NS > 3) each<NL>([&](auto i) QIFT_INLINE { issue(lds2, (k_first + 2) * kBK, i); });
   each<FIRST>([&](auto i) QIFT_INLINE { issue(lds_last, (k_first + NS - 1) * kBK, i); });
   __builtin_amdgcn_sched_barrier(0);
   if constexpr (OT != kAcc) {
@@ -178,7 +175,7 @@ __global__ __launch_bounds__(64 * GN * GM) void k_w8_gemm(const int8_t* __restri
     if (tid < BN) s_sw[tid] = sw_pre;
   }
   __builtin_amdgcn_sched_barrier(0);
-  __builtin_amdgcn_s_waitcnt(waits::encode(AHEAD + FIRST, true));
+  __builtin_amdgcn_s_waitcnt(waits::encode(waits::w8_prologue(NS, NL), true));
   __builtin_amdgcn_s_barrier();
   __builtin_amdgcn_sched_barrier(0);
   each<NR>([&](auto r) QIFT_INLINE { read(lds0, Const<0>(), Const<0>(), r); });
@@ -187,13 +184,9 @@ __global__ __launch_bounds__(64 * GN * GM) void k_w8_gemm(const int8_t* __restri
     step(lds0, lds1, lds_last, kt);
     if constexpr (NS == 2) {
       step(lds1, lds0, lds0, kt + 1);
-    } else if constexpr (NS == 3) {
-      step(lds1, lds2, lds0, kt + 1);
-      step(lds2, lds0, lds1, kt + 2);
     } else {
       step(lds1, lds2, lds0, kt + 1);
-      step(lds2, lds3, lds1, kt + 2);
-      step(lds3, lds0, lds2, kt + 3);
+      step(lds2, lds0, lds1, kt + 2);
     }
   }
   __builtin_amdgcn_s_waitcnt(0x0070);   // the loads past the end have landed before the buffers are used again
@@ -206,7 +199,7 @@ __global__ __launch_bounds__(64 * GN * GM) void k_w8_gemm(const int8_t* __restri
   constexpr int SZ = size_of<OT>(), ROW = 32 * TN * SZ, CH = ROW / 16;
   constexpr int PER = (BN + BM) * kBK / (32 * ROW);   // waves whose rows one of the buffers holds
   static_assert(PER * NS >= NW, "the waves' rows fit the buffers");
-  int8_t* const mine = (wave < PER ? lds0 : wave < 2 * PER ? lds1 : wave < 3 * PER ? lds2 : lds3) + wave % PER * (32 * ROW);
+  int8_t* const mine = (wave < PER ? lds0 : wave < 2 * PER ? lds1 : lds2) + wave % PER * (32 * ROW);
   const int64_t n_wave = n_base + 32 * TN * wn;
   const int64_t NY = OT == kAcc ? (N + 3) & ~int64_t(3) : N;
   constexpr int E = 16 / SZ;

@@ -6,8 +6,6 @@ namespace {
 
 using namespace w8;
 
-constexpr int kGroup = 8;
-
 // A workgroup owns 16 RT weight rows and all the tokens (TT tiles of 16).  Its waves take units of 64 U values of k in turn
 // (unit u is wave u mod NWV's), so that together they read whole pieces of each row; weights and codes go straight to the
 // operands of the 16 x 16 x 64 product (lane (r, g): row or token r, values 16 g .. 16 g + 15 of each 64), the next unit's
@@ -19,8 +17,7 @@ template <int RT, int TT, int U, int NWV, int OT>
 __global__ __launch_bounds__(64 * NWV) void k_w8_rows(const int8_t* __restrict__ W, const uint16_t* __restrict__ sw, int64_t N,
                                                       int K, const int8_t* __restrict__ act, const float* __restrict__ sx,
                                                       int M, void* __restrict__ y, int32_t* __restrict__ acc_out) {
-  constexpr int TG = RT * TT < kGroup ? RT * TT : kGroup;   // tiles whose sums meet at a time
-  __shared__ __align__(16) v4i part[NWV][TG][64];
+  __shared__ __align__(16) v4i part[NWV][RT * TT][64];
   const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t n_base = (int64_t)blockIdx.x * (16 * RT);
@@ -72,25 +69,20 @@ __global__ __launch_bounds__(64 * NWV) void k_w8_rows(const int8_t* __restrict__
     use(u1);
   }
 #pragma unroll
-  for (int p0 = 0; p0 < RT * TT; p0 += TG) {
-    if (p0 > 0) __syncthreads();
+  for (int i = 0; i < RT * TT; ++i) part[wave][i][lane] = acc[i / TT][i % TT];
+  __syncthreads();
+  for (int i = wave; i < RT * TT; i += NWV) {
+    v4i d = part[0][i][lane];
 #pragma unroll
-    for (int i = 0; i < TG; ++i)
-      if (p0 + i < RT * TT) part[wave][i][lane] = acc[(p0 + i) / TT][(p0 + i) % TT];
-    __syncthreads();
-    for (int i = wave; i < TG && p0 + i < RT * TT; i += NWV) {
-      v4i d = part[0][i][lane];
-#pragma unroll
-      for (int w = 1; w < NWV; ++w) d += part[w][i][lane];
-      const int j = (p0 + i) / TT, t = (p0 + i) - j * TT, m = 16 * t + r;
-      const int64_t n0 = n_base + 16 * j + 4 * g;
-      if (m >= M || n0 >= N) continue;
-      const int a[4] = {d[0], d[1], d[2], d[3]};
-      float s4[4];
-      scales4(load_scales(sw, n0, N), s4);
-      store_row<OT>(y, m, n0, N, quad<OT>(a, sx[m], s4));
-      if (acc_out) store_row<kAcc>(acc_out, m, n0, N, quad<kAcc>(a, 0.f, s4));
-    }
+    for (int w = 1; w < NWV; ++w) d += part[w][i][lane];
+    const int j = i / TT, t = i - j * TT, m = 16 * t + r;
+    const int64_t n0 = n_base + 16 * j + 4 * g;
+    if (m >= M || n0 >= N) continue;
+    const int a[4] = {d[0], d[1], d[2], d[3]};
+    float s4[4];
+    scales4(load_scales(sw, n0, N), s4);
+    store_row<OT>(y, m, n0, N, quad<OT>(a, sx[m], s4));
+    if (acc_out) store_row<kAcc>(acc_out, m, n0, N, quad<kAcc>(a, 0.f, s4));
   }
 }
 

@@ -1,4 +1,4 @@
-// Counted waits of the linears that keep direct-to-LDS loads in flight across steps (k_gemm32, k_batch):
+// Counted waits of the linears that keep direct-to-LDS loads in flight across steps (k_gemm32, k_batch, k_w8_gemm):
 // how many of a wave's vector-memory loads may still be outstanding where a step hands its buffer over.
 // Loads return in the order they were sent, so "at most n outstanding" means that all but the last n have
 // landed.  A(k) are the NA loads of step k's activations, W(g) the NW loads of weight line group g (LS
@@ -28,6 +28,12 @@ constexpr int batch_prologue(int NA) { return 3 * NA; }
 constexpr int batch_step(int NA, int NW, int LS, int q, bool more) {
   return LS == 4 && q == 3 ? 3 * NA : 3 * NA + (more ? NW : 0);
 }
+
+// k_w8_gemm, NS buffers, L loads of a step.  Order: A(0) .. A(NS - 2), the first part of A(NS - 1) | per step k: the rest of
+// A(k + NS - 1), the handover of step k, the first part of A(k + NS).
+constexpr int w8_first(int L) { return L / 2; }
+constexpr int w8_prologue(int NS, int L) { return (NS - 2) * L + w8_first(L); }   // A(0) has landed
+constexpr int w8_handover(int NS, int L) { return (NS - 2) * L; }                 // A(k + 1) has
 
 // s_waitcnt operand: vmcnt(n) with expcnt and, unless lgkm0, lgkmcnt left alone
 constexpr int encode(int n, bool lgkm0) { return (lgkm0 ? 0x0070 : 0x0F70) | (n & 15) | ((n >> 4) << 14); }

@@ -139,6 +139,49 @@ def test_no_spills(name, count):
         assert all(v[".group_segment_fixed_size"] <= (81920 if "ILi1E" in k else 163840) for k, v in ks.items())
 
 
+WAITS = """
+#include <cstdio>
+#include "qift_waits.h"
+using namespace qift::waits;
+int main() {
+  int NS, L;
+  while (std::scanf("%d %d", &NS, &L) == 2) std::printf("%d %d %d\\n", w8_first(L), w8_prologue(NS, L), w8_handover(NS, L));
+}
+"""
+
+
+def test_counted_waits(tmp_path):
+    """The loads sent in the tiled product's order: where a step hands its buffer over, the next step's have all landed, and what
+    goes into a buffer goes there after every wave has passed the barrier behind its last read of it."""
+    cxx = shutil.which("g++") or shutil.which("clang++") or "/opt/rocm/llvm/bin/clang++"
+    (tmp_path / "probe.cpp").write_text(WAITS)
+    subprocess.run([cxx, "-std=c++17", "-I", CSRC, str(tmp_path / "probe.cpp"), "-o", str(tmp_path / "probe")], check=True)
+    cases = [(3, 5), (3, 3), (3, 6), (2, 8)]
+    out = subprocess.run([str(tmp_path / "probe")], input="".join("%d %d\n" % c for c in cases), text=True, capture_output=True,
+                         check=True).stdout.splitlines()
+    for (NS, L), line in zip(cases, out):
+        first, prologue, handover = (int(v) for v in line.split())
+        for steps in range(1, 12):
+            sent, landed, done = [], 0, -1
+
+            def send(k, n):
+                assert k - NS <= done, (NS, L, k)                    # the step whose buffer this was has handed it over
+                sent.extend([k] * n)
+
+            for k in range(NS - 1):
+                send(k, L)
+            send(NS - 1, first)
+            landed = max(landed, len(sent) - prologue)
+            for k in range(-(-steps // NS) * NS):
+                assert sent[:landed].count(k) == L, (NS, L, k)       # step k's tiles are there when it reads them
+                send(k + NS - 1, L - first)
+                landed = max(landed, len(sent) - handover)
+                assert sent[:landed].count(k + 1) == L
+                done = k
+                send(k + NS, first)
+            assert 0 <= handover <= prologue < 64
+
+
 def test_oracle_codes_are_the_rationals():
     rng = np.random.default_rng(3)
     X = np.concatenate([rng.normal(0, 1, (3, 16)), rng.integers(-254, 255, (4, 16)) * 0.5, np.zeros((1, 16))])
