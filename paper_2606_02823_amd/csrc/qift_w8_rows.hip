@@ -6,22 +6,24 @@ namespace {
 
 using namespace w8;
 
-// A workgroup owns 16 RT weight rows and all the tokens (TT tiles of 16).  Its waves take units of 64 U values of k in turn
-// (unit u is wave u mod NWV's), so that together they read whole pieces of each row; weights and codes go straight to the
-// operands of the 16 x 16 x 64 product (lane (r, g): row or token r, values 16 g .. 16 g + 15 of each 64), the next unit's
-// loads sent before the present one is used.  The waves' sums meet in LDS, each wave adding up and storing some of the tiles.
-// Bound by the weights' bytes with few tokens (28672 x 4096 at one 24.1 us, 4.9 TB/s; 4096 x 14336 13.5, 4.4; 4096 x 4096 5.9,
+// A workgroup owns `own` weight rows, a multiple of 4 and at most 16 RT, and all the tokens (TT tiles of 16); `own` is chosen
+// so that the CUs have equal parts (6144 x 4096 at one token: 24 rows to each of 256 workgroups 7.2 us, 32 to 192 8.1).  Its
+// waves take units of 64 U values of k in turn (unit u is wave u mod NWV's), so that together they read whole pieces of each
+// row; weights and codes go straight to the operands of the 16 x 16 x 64 product (lane (r, g): row or token r, values 16 g ..
+// 16 g + 15 of each 64), the next unit's loads sent before the present one is used.  The waves' sums meet in LDS, each wave
+// adding up and storing some of the tiles.
+// Bound by the weights' bytes with few tokens (28672 x 4096 at one 24.5 us, 4.8 TB/s; 4096 x 14336 12.9, 4.5; 4096 x 4096 6.0,
 // of which 2.5 are the launch and the first loads), with more by what a CU takes into registers, about 27 bytes a ns
-// (4096 x 4096 at 32 tokens 8.4 us): tiled products (qift_w8_gemm.hip) take over there.
+// (4096 x 4096 at 32 tokens 8.6 us): tiled products (qift_w8_gemm.hip) take over there.
 template <int RT, int TT, int U, int NWV, int OT>
 __global__ __launch_bounds__(64 * NWV) void k_w8_rows(const int8_t* __restrict__ W, const uint16_t* __restrict__ sw, int64_t N,
-                                                      int K, const int8_t* __restrict__ act, const float* __restrict__ sx,
+                                                      int K, int own, const int8_t* __restrict__ act, const float* __restrict__ sx,
                                                       int M, void* __restrict__ y, int32_t* __restrict__ acc_out) {
   __shared__ __align__(16) v4i part[NWV][RT * TT][64];
   const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t n_base = (int64_t)blockIdx.x * (16 * RT);
-  const int rows = (int)(N - n_base < 16 * RT ? N - n_base : 16 * RT);
+  const int64_t n_base = (int64_t)blockIdx.x * own;
+  const int rows = (int)(N - n_base < own ? N - n_base : own);
   const __amdgpu_buffer_rsrc_t wr = dev::make_rsrc(W + n_base * K, (uint32_t)rows * (uint32_t)K);
   const __amdgpu_buffer_rsrc_t ar = dev::make_rsrc(act, (uint32_t)M * (uint32_t)K);
   uint32_t wo[RT], ao[TT];
@@ -77,7 +79,7 @@ __global__ __launch_bounds__(64 * NWV) void k_w8_rows(const int8_t* __restrict__
     for (int w = 1; w < NWV; ++w) d += part[w][i][lane];
     const int j = i / TT, t = i - j * TT, m = 16 * t + r;
     const int64_t n0 = n_base + 16 * j + 4 * g;
-    if (m >= M || n0 >= N) continue;
+    if (m >= M || 16 * j + 4 * g >= rows) continue;
     const int a[4] = {d[0], d[1], d[2], d[3]};
     float s4[4];
     scales4(load_scales(sw, n0, N), s4);
@@ -87,12 +89,12 @@ __global__ __launch_bounds__(64 * NWV) void k_w8_rows(const int8_t* __restrict__
 }
 
 template <int RT, int TT, int U, int NWV>
-hipError_t launch_rows(const W8Call& c, hipStream_t s) {
-  const dim3 grid((unsigned)((c.N + 16 * RT - 1) / (16 * RT)));
+hipError_t launch_rows(const W8Call& c, int rows, hipStream_t s) {
+  const dim3 grid((unsigned)((c.N + rows - 1) / rows));
   auto kernel = c.dtype == kF32    ? k_w8_rows<RT, TT, U, NWV, kF32>
                 : c.dtype == kBF16 ? k_w8_rows<RT, TT, U, NWV, kBF16>
                                    : k_w8_rows<RT, TT, U, NWV, kF16>;
-  hipLaunchKernelGGL(kernel, grid, dim3(64 * NWV), 0, s, c.levels, c.scales, c.N, (int)c.K, c.act, c.sx, (int)c.M, c.out,
+  hipLaunchKernelGGL(kernel, grid, dim3(64 * NWV), 0, s, c.levels, c.scales, c.N, (int)c.K, rows, c.act, c.sx, (int)c.M, c.out,
                      c.acc);
   return hipGetLastError();
 }
@@ -100,13 +102,15 @@ hipError_t launch_rows(const W8Call& c, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_w8_rows(const W8Call& c, const route::W8Plan& p, hipStream_t s) {
-  // longer units where a wave has few (4096 x 14336 at one token 13.5 us against 15.4), shorter ones where many workgroups
-  // share a CU (28672 x 4096 24.1 against 26.7)
   if (c.M <= 16) {
-    if (p.rows == 32) return launch_rows<2, 1, 4, 4>(c, s);
-    return c.N <= 16 * 512 ? launch_rows<1, 1, 4, 8>(c, s) : launch_rows<1, 1, 2, 8>(c, s);
+    // four waves with units of 256 k (4096 x 14336 at one token 12.9 us; eight 13.7; of 128 k 15.6) except where many workgroups
+    // queue for a CU: there eight with units of 128 (28672 x 4096 24.5 against 26.0)
+    if (p.rows > 16) return launch_rows<2, 1, 4, 4>(c, p.rows, s);
+    const bool many = (c.N + p.rows - 1) / p.rows > 2 * route::kCus && c.K > 1024 && c.K <= 8192;
+    return many ? launch_rows<1, 1, 2, 8>(c, p.rows, s) : launch_rows<1, 1, 4, 4>(c, p.rows, s);
   }
-  return p.rows == 16 ? launch_rows<1, 2, 2, 8>(c, s) : p.rows == 32 ? launch_rows<2, 2, 2, 4>(c, s) : launch_rows<4, 2, 2, 4>(c, s);
+  if (p.rows <= 16) return launch_rows<1, 2, 2, 4>(c, p.rows, s);
+  return p.rows <= 32 ? launch_rows<2, 2, 2, 4>(c, p.rows, s) : launch_rows<4, 2, 2, 4>(c, p.rows, s);
 }
 
 }  // namespace qift

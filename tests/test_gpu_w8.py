@@ -109,7 +109,8 @@ def operands(rng, N, K, M):
 
 # up to 64 tokens: every number of token tiles and of row tiles, whole and cut rows of every kind
 ROWS = [(M, N, K) for M in (1, 4, 16, 17, 33, 48, 49, 64) for N, K in ((1, 64), (37, 192), (512, 256), (1027, 448))] + \
-       [(M, N, 320) for M in (2, 30, 47, 61) for N in (8200, 9000, 16403)] + [(3, 130, 8192), (64, 70, 131072)]
+       [(M, N, 320) for M in (2, 30, 47, 61) for N in (8200, 9000, 16403)] + [(3, 130, 8192), (64, 70, 131072)] + \
+       [(M, N, 1088) for M in (1, 16, 17, 32) for N in (1021, 2045, 3069, 5119, 6142, 7165, 9001, 11003, 13001)]   # 4 to 52 rows to a workgroup
 
 
 @pytest.mark.parametrize("M,N,K", ROWS)

@@ -122,12 +122,12 @@ def test_plan_limits(tmp_path):
         assert unsplit == 1 and kind > 0
         assert 1 <= parts <= (K + 127) // 128
         if rows:
-            assert rows in (16, 32, 64) and M <= 32 and parts == 1
+            assert rows % 4 == 0 and 4 <= rows <= (32 if M <= 16 else 64) and M <= 32 and parts == 1
         else:
             assert (bn, bm) in ((128, 32), (128, 64), (256, 128), (256, 256)) and (bm > 32 or M <= 32)
         assert ws == (0 if parts == 1 else parts * M * ((N + 3) // 4 * 4) * 4) and (parts == 1 or M <= 65535)
-        seen.add((rows, bm, parts > 1))
-    assert {(16, 0, False), (32, 0, False), (0, 32, False), (0, 64, True), (0, 128, False), (0, 256, False)} <= seen
+        seen.add((-(-rows // 16) * 16, bm, parts > 1))
+    assert {(16, 0, False), (32, 0, False), (64, 0, False), (0, 32, False), (0, 64, True), (0, 128, False), (0, 256, False)} <= seen
 
 
 @pytest.mark.parametrize("name,count", [("k_w8_rows", 18), ("k_w8_gemm", 16), ("k_w8_sum", 3)])
