@@ -75,6 +75,12 @@ inline W8Plan w8_plan(int64_t N, int64_t M, int64_t K, bool split) {
   }
   return best;
 }
+// Whether the rows kernel takes eight waves with units of 128 k rather than four with units of 256, for up to 16 tokens and 16
+// rows: four (4096 x 14336 at one token 12.9 us; eight 13.7; of 128 k 15.6) except where many workgroups queue for a CU
+// (28672 x 4096 24.5 with eight against 26.0).
+inline bool w8_eight_waves(const W8Plan& p, int64_t N, int64_t K) {
+  return w8_ceil(N, p.rows) > 2 * kCus && K > 1024 && K <= 8192;
+}
 // Bytes of the parts' sums.
 inline size_t w8_workspace(const W8Plan& p, int64_t N, int64_t M) {
   return p.parts == 1 ? 0 : (size_t)p.parts * (size_t)M * (size_t)(w8_ceil(N, 4) * 4) * sizeof(int32_t);

@@ -103,11 +103,8 @@ hipError_t launch_rows(const W8Call& c, int rows, hipStream_t s) {
 
 hipError_t launch_w8_rows(const W8Call& c, const route::W8Plan& p, hipStream_t s) {
   if (c.M <= 16) {
-    // four waves with units of 256 k (4096 x 14336 at one token 12.9 us; eight 13.7; of 128 k 15.6) except where many workgroups
-    // queue for a CU: there eight with units of 128 (28672 x 4096 24.5 against 26.0)
     if (p.rows > 16) return launch_rows<2, 1, 4, 4>(c, p.rows, s);
-    const bool many = (c.N + p.rows - 1) / p.rows > 2 * route::kCus && c.K > 1024 && c.K <= 8192;
-    return many ? launch_rows<1, 1, 2, 8>(c, p.rows, s) : launch_rows<1, 1, 4, 4>(c, p.rows, s);
+    return route::w8_eight_waves(p, c.N, c.K) ? launch_rows<1, 1, 2, 8>(c, p.rows, s) : launch_rows<1, 1, 4, 4>(c, p.rows, s);
   }
   if (p.rows <= 16) return launch_rows<1, 2, 2, 4>(c, p.rows, s);
   return p.rows <= 32 ? launch_rows<2, 2, 2, 4>(c, p.rows, s) : launch_rows<4, 2, 2, 4>(c, p.rows, s);

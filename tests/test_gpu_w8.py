@@ -9,6 +9,7 @@ import numpy as np
 import pytest
 import torch
 
+import w8_cases
 from oracle import hadamard, linear as olin, w8
 
 pytestmark = pytest.mark.gpu
@@ -253,3 +254,28 @@ def test_binding_refuses(Q):
         Q.W8(torch.zeros((8, 64), dtype=torch.int8), torch.zeros(8, dtype=torch.float16, device="cuda"))
     with pytest.raises(Q.QiftError):
         Q.rotate_quant_act8(torch.zeros((4, 96), dtype=torch.float16, device="cuda"), 32)
+
+
+@pytest.mark.parametrize("M,N,K,kernel,parts", w8_cases.CASES)
+def test_linear_of_each_kernel(Q, M, N, K, kernel, parts):
+    """Every kernel in every output type, with the sums and without, results inside a larger array whose ends stay as they were.
+    (The sums are whole numbers below 2^53 in fp64: exact.)"""
+    rng = np.random.default_rng(M + N + K)
+    L, q, s_w, s_x = operands(rng, N, K, M)
+    acc = (q.astype(np.float64) @ L.astype(np.float64).T).astype(np.int64)
+    w, act = Q.W8(dev(L), dev(s_w)), Q.QAct(dev(q), dev(s_x))
+    ws = Q.w8a8_workspace(w, M)
+    assert ws is not None or parts == 1
+    pad = 64
+    for dt in OUT:
+        want = expect(acc, s_x, s_w, dt)
+        got_acc = torch.full((M, N), -7, dtype=torch.int32, device="cuda")
+        if ws is not None:
+            ws.fill_(0x5A)
+        assert same(Q.w8a8_linear(w, act, dtype=dt, acc_out=got_acc, workspace=ws), want), dt
+        assert np.array_equal(got_acc.cpu().numpy(), acc)
+        room = torch.full((2 * pad + M * N,), 7.0, dtype=dt, device="cuda")
+        out = room[pad:pad + M * N].view(M, N)
+        Q.w8a8_linear(w, act, out=out, workspace=ws)
+        assert same(out, want), dt
+        assert torch.all(room[:pad] == 7) and torch.all(room[pad + M * N:] == 7)

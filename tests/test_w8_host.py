@@ -10,6 +10,7 @@ from fractions import Fraction
 import numpy as np
 import pytest
 
+import w8_cases
 from oracle import hadamard, quant, w8
 from paper_2606_02823_amd import qift
 from test_kernel_resources import kernels
@@ -213,3 +214,40 @@ def test_oracle_scales_and_error_bound():
     assert np.all(np.abs(W - d * L) <= d * (0.5 + 127 * 2.0 ** -11))
     assert np.array_equal(w8.epilogue(np.array([[3]]), np.array([0.5]), np.array([2.0])), [[np.float32(3.0)]])
     assert quant.rne(np.array([2.5]))[0] == 2
+
+
+KERNEL = """
+#include <cstdio>
+#include "qift_w8_route.h"
+using namespace qift::route;
+int main() {
+  long N, M, K;
+  while (std::scanf("%ld %ld %ld", &N, &M, &K) == 3) {
+    const W8Plan p = w8_plan(N, M, K, true);
+    if (!p.rows) std::printf("%dx%d:%d\\n", p.bn, p.bm, p.parts);
+    else if (M <= 16) std::printf("rows %dx1x%d:1\\n", p.rows > 16 ? 2 : 1, p.rows <= 16 && w8_eight_waves(p, N, K) ? 8 : 4);
+    else std::printf("rows %dx2x4:1\\n", p.rows > 32 ? 4 : p.rows > 16 ? 2 : 1);
+  }
+}
+"""
+
+
+def test_each_kernel_has_its_sizes(tmp_path):
+    """The sizes that the GPU tests run take the kernels that they are there for: every rows kernel, every tile uncut and cut, the
+    tiles with ragged sides and with K of an odd number of 64s among the uncut ones."""
+    cxx = shutil.which("g++") or shutil.which("clang++") or "/opt/rocm/llvm/bin/clang++"
+    (tmp_path / "probe.cpp").write_text(KERNEL)
+    subprocess.run([cxx, "-std=c++17", "-I", CSRC, str(tmp_path / "probe.cpp"), "-o", str(tmp_path / "probe")], check=True)
+    out = subprocess.run([str(tmp_path / "probe")], input="".join(f"{N} {M} {K}\n" for M, N, K, _, _ in w8_cases.CASES), text=True,
+                         capture_output=True, check=True).stdout.splitlines()
+    assert len(out) == len(w8_cases.CASES)
+    for (M, N, K, name, parts), got in zip(w8_cases.CASES, out):
+        assert got == f"{name}:{parts}", (M, N, K)
+    for rows in w8_cases.ROWS:
+        assert any(c[3] == "rows " + rows for c in w8_cases.CASES), rows
+    for tile in w8_cases.TILES:
+        bn, bm = (int(v) for v in tile.split("x"))
+        whole, cut = ([c for c in w8_cases.CASES if c[3] == tile and (c[4] > 1) == split] for split in (False, True))
+        assert whole and cut, tile
+        assert any(c[1] % bn and c[0] % bm for c in whole) and any(c[1] % bn and c[0] % bm for c in cut), tile
+        assert any(c[2] % 128 == 64 for c in whole), tile
