@@ -44,8 +44,8 @@ extern "C" {
  *   page           tokens of a page, a positive multiple of 16.
  *   rows           entries of slots and positions.
  *   starts out: int32 [B + 1]; lens_out out: int32 [B]; slots, positions out: int32 [rows]; free_out out: int32 [1].
- *   lens_out and free_out are other arrays than lens and free_count (QIFT_ERR_SHAPE for the same pointer): every workgroup
- *   reads those afresh.  A loop of steps has two of each in turn.
+ *   Nothing that is written (the table and the outputs) may overlap another of the arrays, the inputs among them
+ *   (QIFT_ERR_SHAPE): every workgroup reads those afresh.  A loop of steps has two of lens_out and free_out in turn.
  * B = 0 gives starts[0] = 0 and rows of -1.  All arrays 4-byte aligned.  Limits: B <= 65535, rows < 2^31,
  * table_pages * page < 2^31, capacity < 2^31.  One launch.
  */
@@ -61,7 +61,8 @@ int qift_kv4_plan_step(const int32_t *lens, const int32_t *counts, int64_t B, in
  * sequences share are the caller's to count: each row that names one gives it back.
  * A length or depth outside its range is taken as in qift_kv4_plan_step; pages past the stack's capacity are dropped and a
  * negative page number is put back as it is, both with QIFT_DEVERR_INDEX.
- * Arguments, aliasing rule, limits and alignment as there.  B = 0 copies the depth.  One launch.
+ * free_pages, lens_out and free_out are written and overlap nothing else (QIFT_ERR_SHAPE).  Arguments, limits and alignment
+ * as there.  B = 0 copies the depth.  One launch.
  */
 int qift_kv4_release(const int32_t *lens, const int32_t *done, int64_t B, const int32_t *table, int32_t table_pages,
                      int32_t page, int32_t *free_pages, const int32_t *free_count, int64_t capacity, int32_t *lens_out,

@@ -16,6 +16,23 @@ bool tables_ok(int64_t B, int32_t table_pages, int32_t page, int64_t capacity) {
          capacity >= 0 && capacity < k31;
 }
 
+struct Words {   // an array of 32-bit numbers
+  const void* p;
+  int64_t n;
+};
+
+// Whether one of the first `outputs` arrays overlaps any other.  Every workgroup reads the inputs afresh and none waits for
+// another, so such a call's results would depend on their order.
+template <int N>
+bool overlap(const Words (&a)[N], int outputs) {
+  for (int i = 0; i < outputs; ++i)
+    for (int j = i + 1; j < N; ++j) {
+      const uintptr_t x = reinterpret_cast<uintptr_t>(a[i].p), y = reinterpret_cast<uintptr_t>(a[j].p);
+      if (a[i].n > 0 && a[j].n > 0 && x < y + 4 * (uintptr_t)a[j].n && y < x + 4 * (uintptr_t)a[i].n) return true;
+    }
+  return false;
+}
+
 }  // namespace
 
 extern "C" {
@@ -32,6 +49,9 @@ int qift_kv4_plan_step(const int32_t* lens, const int32_t* counts, int64_t B, in
   const void* p[] = {lens, counts, table, free_pages, free_count, starts, lens_out, slots, positions, free_out};
   for (const void* x : p)
     if (!aligned(x, 4)) return QIFT_ERR_ALIGN;
+  const Words arrays[] = {{table, B * table_pages}, {starts, B + 1}, {lens_out, B}, {slots, rows}, {positions, rows}, {free_out, 1},
+                          {lens, B}, {counts, B}, {free_pages, capacity}, {free_count, 1}};
+  if (overlap(arrays, 6)) return QIFT_ERR_SHAPE;
   return qift::report_hip(qift::launch_plan_step({lens, counts, table, free_pages, free_count, starts, lens_out, slots, positions,
                                                   free_out, B, rows, capacity, table_pages, page},
                                                  (hipStream_t)stream));
@@ -47,6 +67,9 @@ int qift_kv4_release(const int32_t* lens, const int32_t* done, int64_t B, const 
   const void* p[] = {lens, done, table, free_pages, free_count, lens_out, free_out};
   for (const void* x : p)
     if (!aligned(x, 4)) return QIFT_ERR_ALIGN;
+  const Words arrays[] = {{free_pages, capacity}, {lens_out, B}, {free_out, 1}, {lens, B}, {done, B}, {table, B * table_pages},
+                          {free_count, 1}};
+  if (overlap(arrays, 3)) return QIFT_ERR_SHAPE;
   return qift::report_hip(qift::launch_release(
       {lens, done, table, free_pages, free_count, lens_out, free_out, B, capacity, table_pages, page}, (hipStream_t)stream));
 }

@@ -670,8 +670,8 @@ def kv4_plan_step(lens: torch.Tensor, counts: torch.Tensor, table: torch.Tensor,
                   free_count: torch.Tensor, page: int, rows: int, out: KV4Plan | None = None, stream=None) -> KV4Plan:
     """Slots, positions, row starts and new lengths of counts[b] new tokens for each of B sequences with lens[b] cached
     ones (int32 [B]), their pages taken from the top of the stack free_pages[: free_count] (int32 [capacity], [1]) into
-    table (int32 [B, table_pages], written in place).  rows: how many rows the step has room for.  What out names must be
-    other tensors than lens and free_count."""
+    table (int32 [B, table_pages], written in place).  rows: how many rows the step has room for.  The table and what out
+    names must not overlap each other or the inputs."""
     B, width, index = _step_tables(lens, counts, table, free_pages, free_count, "counts")
     if out is None:   # one piece of memory for the five
         out = KV4Plan(*_empty_of(table, 2 * B + 2 * rows + 2, stream).split_with_sizes((B + 1, B, rows, rows, 1)))
@@ -693,7 +693,7 @@ def kv4_plan_step(lens: torch.Tensor, counts: torch.Tensor, table: torch.Tensor,
 def kv4_release(lens: torch.Tensor, done: torch.Tensor, table: torch.Tensor, free_pages: torch.Tensor, free_count: torch.Tensor,
                 page: int, out=None, stream=None):
     """The pages of the sequences with done[b] != 0 (int32 [B]) put back on the stack (free_pages, written in place).
-    Returns (lens, free_count) after that, new tensors or the pair out."""
+    Returns (lens, free_count) after that, new tensors or the pair out, which must not overlap the inputs."""
     B, width, index = _step_tables(lens, done, table, free_pages, free_count, "done")
     if out is None:
         out = _empty_of(table, B + 1, stream).split_with_sizes((B, 1))

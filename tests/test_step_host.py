@@ -256,3 +256,35 @@ def test_oracle_rotation():
         z, _ = ostep.head_norm_rope(y[1:2], None, 1e-6, freq, np.array([995]), 96, pairs)
         direct, _ = ostep.head_norm_rope(x[1:2], w, 1e-6, freq, np.array([1000]), 96, pairs)
         assert np.allclose(z, direct, atol=1e-12)
+
+
+def _apart(call, sizes, outputs):
+    """call with every array in a place of its own, then each output laid over each other array, at its first entry and at its last."""
+    at, place = 0x100000, {}
+    for name, n in sizes.items():
+        place[name] = at
+        at += 4 * n + 4096
+    for out in outputs:
+        for name in sizes:
+            if name == out:
+                continue
+            for move in (place[name], place[name] + 4 * (sizes[name] - 1), place[name] - 4 * (sizes[out] - 1)):
+                assert call({**place, out: move}) == E_SHAPE, (out, name, move - place[name])
+
+
+def test_outputs_lie_apart(L):
+    """Every workgroup reads the inputs afresh and nothing orders the outputs: no output may overlap another array."""
+    B, width, cap, rows = 300, 3, 70, 900
+
+    def plan(p):
+        return L.qift_kv4_plan_step(p["lens"], p["counts"], B, p["table"], width, 16, p["free"], p["depth"], cap, rows, p["starts"],
+                                    p["lens_out"], p["slots"], p["positions"], p["free_out"], None)
+
+    def release(p):
+        return L.qift_kv4_release(p["lens"], p["done"], B, p["table"], width, 16, p["free"], p["depth"], cap, p["lens_out"],
+                                  p["free_out"], None)
+
+    _apart(plan, {"lens": B, "counts": B, "table": B * width, "free": cap, "depth": 1, "starts": B + 1, "lens_out": B, "slots": rows,
+                     "positions": rows, "free_out": 1}, ("table", "starts", "lens_out", "slots", "positions", "free_out"))
+    _apart(release, {"lens": B, "done": B, "table": B * width, "free": cap, "depth": 1, "lens_out": B, "free_out": 1},
+           ("free", "lens_out", "free_out"))
