@@ -72,7 +72,8 @@ int qift_kv4_release(const int32_t *lens, const int32_t *done, int64_t B, const 
  * Norms and rotation of a model's heads (host; a non-owning view).
  *   rot        values of each head that are rotated, its first ones: a multiple of 8, 0 .. head_dim.
  *   pairs      0: value i is paired with value i + rot / 2; 1: value 2 i with value 2 i + 1.
- *   freq       fp32 [rot / 2], finite: the angle of pair i at position p is p * freq[i].
+ *   freq       fp32 [rot / 2]: the angle of pair i at position p is p * freq[i].  Angles are below 2^40 (for every position:
+ *              |freq| < 512); a pair whose angle is not, or whose frequency is no number, gets NaN.
  *   q_weight, k_weight   [head_dim] in the type of the rows, nullable: without one those heads are not normed.
  *   eps        finite, at least 2^-80 (squares that fp32 cannot hold are then nothing beside it).
  */
@@ -88,7 +89,7 @@ typedef struct {
  * For each head x of a row at position p:
  *   y = x / sqrt(mean(x^2) + eps) * w      (y = x without a weight)
  *   (a, b) -> (a cos t - b sin t, a sin t + b cos t), t = p * freq[i], for each pair of the rotated values.
- * fp32, the angle reduced in fp64 (sine and cosine are within 2^-22 for every position), one rounding at the end.  The result
+ * fp32, the angle's exact product reduced in fp64 (sine and cosine are within 2^-22), one rounding at the end.  The result
  * is within half a step of its type and 2^-19 (|a| + |b|) of the exact one, a and b the pair's normed values.  The sum
  * of a head's squares has to be finite in fp32.
  *   q, k        fp16 or bf16: row r, head h starts at element r * stride + 128 h; strides multiples of 8 and at least

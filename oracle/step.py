@@ -68,8 +68,9 @@ def head_norm_rope(x, weight, eps, freq, positions, rot, pairs):
     x = np.asarray(x, np.float64)
     if weight is not None:
         x = x / np.sqrt((x * x).mean(axis=-1, keepdims=True) + float(np.float32(eps))) * np.asarray(weight, np.float64)
-    angle = np.asarray(positions, np.float64)[:, None] * np.asarray(freq, np.float32).astype(np.float64)[None, :]
-    cos, sin = np.cos(angle)[:, None, :], np.sin(angle)[:, None, :]
+    # (64 bits of mantissa hold the product of a position and an fp32 frequency)
+    angle = np.asarray(positions, np.longdouble)[:, None] * np.asarray(freq, np.float32).astype(np.longdouble)[None, :]
+    cos, sin = (f(angle).astype(np.float64)[:, None, :] for f in (np.cos, np.sin))
     half = rot // 2
     i = np.arange(half)
     first, second = (2 * i, 2 * i + 1) if pairs else (i, i + half)

@@ -2,8 +2,8 @@
 //
 //   y = x / sqrt(mean(x^2) + eps) * w      over the 128 values of a head (no weight: y = x)
 //   (a, b) -> (a cos t - b sin t, a sin t + b cos t),  t = position * freq[i]
-// for the pairs i of the first rot values: values i and i + rot / 2, or 2 i and 2 i + 1.  fp32 throughout, the angle in fp64;
-// one rounding at the end.
+// for the pairs i of the first rot values: values i and i + rot / 2, or 2 i and 2 i + 1.  fp32 throughout, the angle in fp64
+// (step::turn); one rounding at the end.
 #include "qift_fwht.h"
 #include "qift_internal.h"
 #include "qift_step.h"
@@ -22,29 +22,6 @@ __device__ __forceinline__ float row_sum(float x) {
   QIFT_ADD(0x140);   // row_mirror
 #undef QIFT_ADD
   return x;
-}
-
-// Sine and cosine of position * freq: the product is exact in fp64 for positions below 2^29, the remainder of its
-// division by pi / 2 is taken with pi / 2 in two parts (off by less than 2^-80 of a quadrant for each), and the Taylor
-// sums of the remainder, |r| <= pi / 4, are cut where the next term is below 2^-29.
-__device__ __forceinline__ void turn(int32_t position, float freq, float& sine, float& cosine) {
-  const double x = (double)position * (double)freq;
-  const double n = rint(x * 0x1.45f306dc9c883p-1);                       // 2 / pi
-  const double r = fma(-n, 0x1.1a62633145c07p-54, fma(-n, 0x1.921fb54442d18p0, x));
-  const int quadrant = (int)(n - 4.0 * floor(n * 0.25));
-  const float f = (float)r, z = f * f;
-  float s = fmaf(z, 1.f / 362880.f, -1.f / 5040.f);
-  s = fmaf(s, z, 1.f / 120.f);
-  s = fmaf(s, z, -1.f / 6.f);
-  s = fmaf(s * z, f, f);
-  float c = fmaf(z, -1.f / 3628800.f, 1.f / 40320.f);
-  c = fmaf(c, z, -1.f / 720.f);
-  c = fmaf(c, z, 1.f / 24.f);
-  c = fmaf(c, z, -0.5f);
-  c = fmaf(c, z, 1.f);
-  const float a = quadrant & 1 ? c : s, b = quadrant & 1 ? s : c;
-  sine = quadrant & 2 ? -a : a;
-  cosine = (quadrant + 1) & 2 ? -b : b;
 }
 
 template <bool BF16>
@@ -109,7 +86,7 @@ __global__ __launch_bounds__(256) void k_rope(RopeCall c, pages::Div per_row, ui
     u[i][1] = *reinterpret_cast<const uint2*>(from + at1);
   }
   float sine = 0.f, cosine = 1.f;
-  if (turns) turn(position, c.freq[4 * l + g], sine, cosine);
+  if (turns) step::turn(position, c.freq[4 * l + g], sine, cosine);
   float s[4], co[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {

@@ -1,6 +1,8 @@
 // Arithmetic of a serving step's plan, for the kernels and for host code (plain C++: compiled without a GPU too).
 #pragma once
 
+#include <math.h>
+
 #include "qift_pages.h"
 
 namespace qift {
@@ -66,6 +68,33 @@ QIFT_HD Head head_of(int32_t h, int32_t Hq, int32_t Hkv) {
   const int32_t all = Hq + Hkv, in = h < all ? h : all - 1;
   const bool key = in >= Hq;
   return {key ? in - Hq : in, h < all, key};
+}
+
+// Sine and cosine of position * freq, within 2^-22 for angles below kMaxAngle; NaN from there on and for a frequency that is no
+// number.  The product is x + low exactly (55 bits at most), the remainder of x's division by pi / 2 is taken with pi / 2 in
+// two parts (off by less than 2^-51), and the Taylor sums of the remainder, |r| <= pi / 4 + 2^-12, are cut where the next term is
+// below 2^-29.
+constexpr double kMaxAngle = 0x1p40;
+QIFT_HD void turn(int32_t position, float freq, float& sine, float& cosine) {
+  const double product = (double)position * (double)freq;
+  const bool in = fabs(product) < kMaxAngle;
+  const double x = in ? product : 0.0, low = in ? fma((double)position, (double)freq, -product) : 0.0;
+  const double n = rint(x * 0x1.45f306dc9c883p-1);                       // 2 / pi
+  const double r = fma(-n, 0x1.1a62633145c07p-54, fma(-n, 0x1.921fb54442d18p0, x)) + low;
+  const int quadrant = (int)(n - 4.0 * floor(n * 0.25));
+  const float f = (float)r, z = f * f;
+  float s = fmaf(z, 1.f / 362880.f, -1.f / 5040.f);
+  s = fmaf(s, z, 1.f / 120.f);
+  s = fmaf(s, z, -1.f / 6.f);
+  s = fmaf(s * z, f, f);
+  float c = fmaf(z, -1.f / 3628800.f, 1.f / 40320.f);
+  c = fmaf(c, z, -1.f / 720.f);
+  c = fmaf(c, z, 1.f / 24.f);
+  c = fmaf(c, z, -0.5f);
+  c = fmaf(c, z, 1.f);
+  const float a = quadrant & 1 ? c : s, b = quadrant & 1 ? s : c;
+  sine = !in ? NAN : quadrant & 2 ? -a : a;
+  cosine = !in ? NAN : (quadrant + 1) & 2 ? -b : b;
 }
 
 }  // namespace step

@@ -710,8 +710,9 @@ def kv4_release(lens: torch.Tensor, done: torch.Tensor, table: torch.Tensor, fre
 
 class HeadRope:
     """Norms and rotation of a model's heads (qift_head_rope): freq fp32 [rot / 2], the weights [128] in the rows' type or
-    None (not normed); pairs: values 2 i and 2 i + 1 are paired, else i and i + rot / 2.  The object keeps the tensors alive and
-    holds the C view, checked once here."""
+    None (not normed); pairs: values 2 i and 2 i + 1 are paired, else i and i + rot / 2.  Angles (position * freq) are below
+    2^40; a pair past that, or of a frequency that is no number, gets NaN.  The object keeps the tensors alive and holds the C
+    view, checked once here."""
 
     def __init__(self, freq: torch.Tensor, rot: int = 128, pairs: bool = False, q_weight: torch.Tensor | None = None,
                  k_weight: torch.Tensor | None = None, eps: float = 1e-5):

@@ -465,3 +465,34 @@ def test_other_streams(Q):
         assert torch.equal(p.starts, p2.starts) and torch.equal(p.positions, p2.positions) and torch.equal(p.lens, p2.lens)
         assert torch.equal(p.slots, p2.slots) and torch.equal(p.free_count, p2.free_count)
         assert torch.equal(r[0], p.lens) and torch.equal(r[1], p.free_count)
+
+
+@pytest.mark.parametrize("pairs", [False, True])
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_large_frequencies(Q, dtype, pairs):
+    """Angles that fp64 does not hold, up to 2^40; NaN in the pairs past that and nowhere else."""
+    rng = np.random.default_rng(31)
+    pos = np.array([0, 1, 1000, 100000, 523018516, 1639311774, 2142287670, I31])
+    q, k = heads_of(rng, len(pos), 3, dtype), heads_of(rng, len(pos), 2, dtype)
+    freq = np.exp(rng.uniform(-8, 6.2, 64)).astype(np.float32)
+    freq[:4] = 2.6565, 96.7, -511.9, 0.0
+    rope = Q.HeadRope(dev(freq, torch.float32), 128, pairs)
+    yq, yk = Q.head_norm_rope(rope, q.cuda(), k.cuda(), dev(pos))
+    check_rope(yq, q, None, 1.0, freq, pos, 128, pairs)
+    check_rope(yk, k, None, 1.0, freq, pos, 128, pairs)
+    wide = freq.copy()
+    wide[5], wide[9], wide[12], wide[13] = 1e9, np.inf, np.nan, 1e30
+    y = Q.head_norm_rope(Q.HeadRope(dev(wide, torch.float32), 128, pairs), q.cuda(), k.cuda(), dev(pos))[0]
+    with np.errstate(invalid="ignore"):
+        lost = ~(np.abs(pos[:, None].astype(np.float64) * wide.astype(np.float64)[None, :]) < 2.0 ** 40)   # (none beside the border)
+    values = np.zeros((len(pos), 128), bool)
+    i = np.arange(64)
+    for at in ((2 * i, 2 * i + 1) if pairs else (i, i + 64)):
+        values[:, at] = lost
+    gone = torch.from_numpy(values)[:, None, :].expand(-1, 3, -1)
+    assert torch.equal(torch.isnan(y.cpu()), gone)
+    same = np.abs(freq - wide) == 0
+    keep = np.zeros(128, bool)
+    for at in ((2 * i, 2 * i + 1) if pairs else (i, i + 64)):
+        keep[at] = same
+    assert torch.equal(y.cpu()[:, :, torch.from_numpy(keep)], yq.cpu()[:, :, torch.from_numpy(keep)])

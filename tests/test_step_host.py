@@ -5,6 +5,7 @@ import os
 import re
 import shutil
 import subprocess
+from fractions import Fraction
 
 import numpy as np
 import pytest
@@ -288,3 +289,60 @@ def test_outputs_lie_apart(L):
                      "positions": rows, "free_out": 1}, ("table", "starts", "lens_out", "slots", "positions", "free_out"))
     _apart(release, {"lens": B, "done": B, "table": B * width, "free": cap, "depth": 1, "lens_out": B, "free_out": 1},
            ("free", "lens_out", "free_out"))
+
+
+TURN = r"""
+#include <cstdio>
+#include "qift_step.h"
+int main() {
+  int position;
+  float freq, s, c;
+  while (std::scanf("%d %a", &position, &freq) == 2) {
+    qift::step::turn(position, freq, s, c);
+    std::printf("%a %a\n", (double)s, (double)c);
+  }
+}
+"""
+PI = Fraction("3.14159265358979323846264338327950288419716939937510582097494459230781640628620899862803482534211706798")
+
+
+def exact_turn(position, freq):
+    """Sine and cosine of position * freq to 70 digits and more of the angle."""
+    x = position * Fraction(float(freq))
+    r = x - 2 * PI * round(x / (2 * PI))
+    r = Fraction(round(r * 2 ** 200), 2 ** 200)
+    term, s, c = Fraction(1), Fraction(0), Fraction(0)
+    for k in range(40):
+        part = term if k % 4 < 2 else -term
+        if k % 2:
+            s += part
+        else:
+            c += part
+        term = Fraction(round(term * r * 2 ** 200), 2 ** 200) / (k + 1)
+    return float(s), float(c)
+
+
+def test_sine_and_cosine_of_every_angle(tmp_path):
+    """Within 2^-22 for every angle below 2^40, whether or not fp64 holds it; NaN from there on and for frequencies that are no number."""
+    cxx = shutil.which("g++") or shutil.which("clang++") or "/opt/rocm/llvm/bin/clang++"
+    (tmp_path / "probe.cpp").write_text(TURN)
+    subprocess.run([cxx, "-std=c++17", "-I", CSRC, str(tmp_path / "probe.cpp"), "-o", str(tmp_path / "probe")], check=True)
+    rng = np.random.default_rng(17)
+    cases = [(p, np.float32(f)) for p in (0, 1, 7, 100000, 2 ** 24 + 1, 2 ** 28, 1639311774, 2142287670, I31)
+             for f in (0.0, 1e-38, 1e-3, 0.1, 1.0, 2.6565, 96.7, 100.7, -100.7, 511.0, 1e6, 1e9, 9.8e8, 1e12, 1e30, np.inf, np.nan)]
+    cases += [(int(p), np.float32(np.exp(f))) for p, f in zip(rng.integers(0, I31, 3000), rng.uniform(-12, 6.2, 3000))]
+    # angles beside the borders of the quadrants: position 1, and far ones
+    for n in list(range(1, 40)) + [int(v) for v in rng.integers(1, 2 ** 33, 400)]:
+        p = int(rng.integers(1, I31))
+        cases += [(1, np.nextafter(np.float32(n * float(PI) / 4), np.float32(side))) for side in (0, 1e30)]
+        cases += [(p, np.float32(n * float(PI) / 4 / p))]
+    out = subprocess.run([str(tmp_path / "probe")], input="".join(f"{p} {float(f).hex()}\n" for p, f in cases), text=True,
+                         capture_output=True, check=True).stdout.splitlines()
+    assert len(out) == len(cases)
+    for (p, f), line in zip(cases, out):
+        s, c = (float.fromhex(v) for v in line.split())
+        if not np.isfinite(f) or p * abs(Fraction(float(f))) >= 2 ** 40:
+            assert np.isnan(s) and np.isnan(c), (p, f)
+        else:
+            want = exact_turn(p, f)
+            assert abs(s - want[0]) <= 2.0 ** -22 and abs(c - want[1]) <= 2.0 ** -22, (p, f)
