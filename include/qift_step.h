@@ -100,7 +100,7 @@ typedef struct {
  *   q_out, k_out   out: as q and k, with strides of their own; the input itself with the input's stride is taken (each
  *               value is read before it is written), any other overlap is not: the same pointer with another stride, q_out
  *               at k, k_out at q or both outputs at one place are QIFT_ERR_SHAPE.
- * 16-byte aligned, positions 4.  rows = 0 does nothing.  Limits: rows * ceil((Hq + Hkv) / 4) < 2^26.  One launch.
+ * 16-byte aligned, positions 4.  rows = 0 does nothing.  Limits: rows * ceil((Hq + Hkv) / 4) <= 2^26 - 4.  One launch.
  */
 int qift_head_norm_rope(const qift_head_rope *rope, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
                         int32_t dtype, const int32_t *positions, int64_t rows, int32_t Hq, int32_t Hkv, void *q_out,

@@ -83,7 +83,7 @@ int qift_head_norm_rope(const qift_head_rope* rope, const void* q, int64_t q_str
   if ((rope->pairs != 0 && rope->pairs != 1) || !(rope->eps >= 0x1p-80f) || !isfinite(rope->eps)) return QIFT_ERR_SPEC;
   if (rows < 0 || Hq < 0 || Hkv < 0 || Hq > 65535 || Hkv > 65535 || Hq + Hkv < 1) return QIFT_ERR_SHAPE;
   const int64_t groups = (Hq + Hkv + 3) / 4;
-  if (rows >= k31 || rows * groups >= (int64_t(1) << 26)) return QIFT_ERR_SHAPE;
+  if (rows >= k31 || rows * groups + 3 >= (int64_t(1) << 26)) return QIFT_ERR_SHAPE;   // four waves to a workgroup: fewer than 2^32 threads
   const int64_t strides[] = {q_stride, q_out_stride, k_stride, k_out_stride};
   const void* rowsp[] = {q, q_out, k, k_out};
   for (int i = 0; i < 4; ++i) {

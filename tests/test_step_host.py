@@ -346,3 +346,11 @@ def test_sine_and_cosine_of_every_angle(tmp_path):
         else:
             want = exact_turn(p, f)
             assert abs(s - want[0]) <= 2.0 ** -22 and abs(c - want[1]) <= 2.0 ** -22, (p, f)
+
+
+def test_rope_launches_have_fewer_than_2_32_threads(L):
+    """Workgroups of four waves, a wave to each row here: 2^26 - 3 rows and more would round up to 2^32 threads."""
+    r = qift.HeadRopeC(128, 128, 0, 1e-5, A, None, None)
+    for rows in (2 ** 26 - 3, 2 ** 26 - 1):
+        for Hq in (1, 4):
+            assert L.qift_head_norm_rope(ctypes.byref(r), A, 512, None, 0, 0, A, rows, Hq, 0, A, 512, None, 0, None) == E_SHAPE
