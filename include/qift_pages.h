@@ -113,6 +113,9 @@ size_t qift_kv4_attention_tree_workspace_bytes(int64_t B, int32_t Hq, int32_t Hk
  *   lens       int32 [B], n_b <= lens[b] <= max_len and lens[b] <= table_pages * page.  A length
  *              outside [0, that limit] is taken as the nearer end, QIFT_DEVERR_INDEX; for lens[b] < n_b
  *              the nodes past lens[b] have no position and are not seen.
+ *              The new tokens have to be counted: of a sequence whose tokens were not written (one that
+ *              qift_kv4_plan_step left out, whose length stays) the last n_b cached ones are taken for
+ *              them, and its rows of out mean nothing.
  *   max_nodes, max_len   host: what n_b and lens[b] may reach in this call (they size the launch and
  *              the workspace, so a captured call serves any content up to them).
  *              They also decide how work is cut: from 1024 on of B * Hkv * ceil(max_nodes * Hq / Hkv / 32)

@@ -35,7 +35,10 @@ extern "C" {
  * A sequence is served whole or not at all.  Left out, with QIFT_DEVERR_INDEX, are: one whose tokens do not fit its row of
  * the table; one whose rows do not all lie below `rows`; one that needs pages where the stack does not hold them after
  * all the sequences before it (left out for their rows or for pages or not) have had theirs.  Its slots and positions
- * are -1, its lens_out is lens[b], and it takes no pages; its rows keep their places.  A negative count counts as 0 and a
+ * are -1, its lens_out is lens[b], and it takes no pages; its rows keep their places.  What the rest of the step makes of
+ * those rows means nothing: qift_kv4_attention_tree has no way to see that they were left out, takes the last cached tokens for
+ * them and fills their rows of its output.  A sequence has its outputs in this step where lens_out[b] is lens[b] + counts[b],
+ * a row where its position is not negative; the others' outputs do not depend on what was left out.  A negative count counts as 0 and a
  * length outside [0, table_pages * page] as the nearer end (its sequence is left out), with QIFT_DEVERR_INDEX; so does a depth
  * outside [0, capacity].  A page number that is negative or whose slots have no 31 bits gives slots of -1 and QIFT_DEVERR_INDEX.
  *   lens, counts   int32 [B].

@@ -671,7 +671,8 @@ def kv4_plan_step(lens: torch.Tensor, counts: torch.Tensor, table: torch.Tensor,
     """Slots, positions, row starts and new lengths of counts[b] new tokens for each of B sequences with lens[b] cached
     ones (int32 [B]), their pages taken from the top of the stack free_pages[: free_count] (int32 [capacity], [1]) into
     table (int32 [B, table_pages], written in place).  rows: how many rows the step has room for.  The table and what out
-    names must not overlap each other or the inputs."""
+    names must not overlap each other or the inputs.  A sequence that finds no room (rows, pages, its row of the table) is left
+    out whole: positions and slots of -1, its length as it was; what the attention then writes into its rows means nothing."""
     B, width, index = _step_tables(lens, counts, table, free_pages, free_count, "counts")
     if out is None:   # one piece of memory for the five
         out = KV4Plan(*_empty_of(table, 2 * B + 2 * rows + 2, stream).split_with_sizes((B + 1, B, rows, rows, 1)))

@@ -496,3 +496,45 @@ def test_large_frequencies(Q, dtype, pairs):
     for at in ((2 * i, 2 * i + 1) if pairs else (i, i + 64)):
         keep[at] = same
     assert torch.equal(y.cpu()[:, :, torch.from_numpy(keep)], yq.cpu()[:, :, torch.from_numpy(keep)])
+
+
+def test_a_step_that_leaves_a_sequence_out(Q):
+    """The others' outputs are those of a step without it; its rows are told by their positions, and it by its length."""
+    rng = np.random.default_rng(41)
+    B, Hq, Hkv, page, width, out_at = 5, 8, 2, 16, 6, 2
+    cached, counts = np.array([40, 3, 33, 0, 70]), np.array([2, 1, 30, 5, 1])
+    s = Server(rng, cached, width, page, 6)
+    counts[out_at] = width * page - cached[out_at] + 1      # one more than its row of the table holds
+    rows = int(counts.sum()) + 3
+    rope = Q.HeadRope(dev(frequencies(128), torch.float32))
+    n = len(s.free) * page
+    fill = [torch.from_numpy(rng.normal(0, 1, (n, Hkv, 128))).half().cuda() for _ in range(2)]
+    new = [torch.from_numpy(rng.normal(0, 1, (rows, h, 128))).half().cuda() for h in (Hq, Hkv, Hkv)]
+    results = []
+    for without in (False, True):
+        cache = Q.KV4Pages.empty(len(s.free), page, Hkv)
+        Q.kv4_append(cache, *fill, dev(np.arange(n)))
+        table, free = dev(s.table), dev(s.free)
+        c = counts.copy()
+        c[out_at] = 0 if without else c[out_at]
+        Q.device_error()
+        p = Q.kv4_plan_step(dev(s.lens), dev(c), table, free, dev([s.depth]), page, rows)
+        assert Q.device_error() == (0 if without else Q.DEVERR_INDEX)
+        starts, pos, lens = (t.cpu().numpy() for t in (p.starts, p.positions, p.lens))
+        # the same tokens, at the rows that the step gives them
+        take = np.zeros(rows, np.int64)
+        first = np.concatenate([[0], np.cumsum(counts)])
+        for b in range(B):
+            take[starts[b]:starts[b + 1]] = first[b] + np.arange(c[b])
+        q, k, v = (t[torch.from_numpy(take).cuda()].contiguous() for t in new)
+        q, k = Q.head_norm_rope(rope, q, k, p.positions)
+        Q.kv4_append(cache, k, v, p.slots)
+        out = Q.kv4_attention_tree(q, cache, table, p.starts, p.lens, max_nodes=64, max_len=width * page)
+        assert Q.device_error() == 0
+        served = lens == cached + c
+        assert served.tolist() == [b != out_at or without for b in range(B)] and lens[out_at] == cached[out_at]
+        for b in range(B):
+            assert np.all((pos[starts[b]:starts[b + 1]] >= 0) == served[b])
+        results.append([out[starts[b]:starts[b + 1]] for b in range(B) if b != out_at] + [p.free_count, table])
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
