@@ -538,3 +538,31 @@ def test_a_step_that_leaves_a_sequence_out(Q):
         results.append([out[starts[b]:starts[b + 1]] for b in range(B) if b != out_at] + [p.free_count, table])
     for a, b in zip(*results):
         assert torch.equal(a, b)
+
+
+def test_steps_on_several_streams(Q):
+    """Plan, norms and release of three servers, each on a stream of its own; everything that the calls read is made, and waited
+    for, before the first of them, and kept until the last is done."""
+    rng = np.random.default_rng(6)
+    rope = Q.HeadRope(dev(frequencies(128), torch.float32))
+    streams, cases, results = [torch.cuda.Stream() for _ in range(3)], [], []
+    for _ in streams:
+        q, k = heads_of(rng, 900, 8, torch.float16).cuda(), heads_of(rng, 900, 2, torch.float16).cuda()
+        srv = Server(rng, rng.integers(0, 50, 300), 6, 16, 900)
+        counts, done = rng.integers(0, 4, 300), rng.integers(0, 2, 300)
+        cases.append((srv, counts, done, q, k, [dev(t) for t in (srv.lens, counts, done, srv.table, srv.free, [srv.depth])]))
+    torch.cuda.synchronize()
+    for s, (_, _, _, q, k, (lens, counts, done, table, free, depth)) in zip(streams, cases):
+        p = Q.kv4_plan_step(lens, counts, table, free, depth, 16, 900, stream=s)
+        y = Q.head_norm_rope(rope, q, k, p.positions, stream=s)
+        r = Q.kv4_release(p.lens, done, table, free, p.free_count, 16, stream=s)
+        results.append((p, y, r))
+    torch.cuda.synchronize()
+    for (p, y, r), (srv, counts, done, q, k, (_, _, _, table, free, _)) in zip(results, cases):
+        want = ostep.plan(srv.lens, counts, srv.table, srv.free, srv.depth, 16, 900)
+        assert np.array_equal(p.slots.cpu().numpy(), want[3]) and np.array_equal(p.positions.cpu().numpy(), want[4])
+        assert np.array_equal(table.cpu().numpy(), want[2])
+        back = ostep.release(want[1], done, want[2], srv.free, want[5], 16)
+        assert np.array_equal(r[0].cpu().numpy(), back[0]) and np.array_equal(free.cpu().numpy(), back[1]) and int(r[1]) == back[2]
+        again = Q.head_norm_rope(rope, q, k, p.positions)
+        assert torch.equal(y[0], again[0]) and torch.equal(y[1], again[1])
