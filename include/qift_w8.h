@@ -52,7 +52,8 @@ int qift_rotate_quant_act8(const uint16_t *x, int64_t M, qift_hadamard_spec spec
                            qift_stream_t stream);
 
 /* Workspace bytes of qift_w8a8_linear for these weights and M tokens (host query; 0 where it needs none, and for an
- * unsupported shape).  It is not monotonic in M: ask for each M, or take the largest of those that occur. */
+ * unsupported shape).  It is not monotonic in M (K is cut where that is faster): a server asks
+ * once for each M that occurs and takes the largest, which serves them all. */
 size_t qift_w8a8_workspace_bytes(const qift_w8 *w, int64_t M);
 
 /*

@@ -912,12 +912,16 @@ def rotate_quant_act8(x: torch.Tensor, block: int, clip=(1, 1), out: QAct | None
     return out
 
 
-def w8a8_workspace_bytes(w: W8, M: int) -> int:
-    return int(lib().qift_w8a8_workspace_bytes(w._ref, M))
+def w8a8_workspace_bytes(w: W8, M) -> int:
+    """Bytes for M tokens, or the most of several numbers of tokens (an iterable): the need falls and rises with M, so a server
+    whose steps have 1 to n tokens asks for range(1, n + 1) once."""
+    f = lib().qift_w8a8_workspace_bytes
+    return max((int(f(w._ref, m)) for m in M), default=0) if hasattr(M, "__iter__") else int(f(w._ref, M))
 
 
-def w8a8_workspace(w: W8, M: int, stream=None) -> torch.Tensor | None:
-    """A workspace for w8a8_linear calls with these weights and M tokens (one call at a time); None where it needs none."""
+def w8a8_workspace(w: W8, M, stream=None) -> torch.Tensor | None:
+    """A workspace for w8a8_linear calls with these weights and M tokens, or any of several numbers of tokens (one call at a
+    time); None where none needs any."""
     need = w8a8_workspace_bytes(w, M)
     return _empty((need,), torch.uint8, w.device, stream) if need else None
 

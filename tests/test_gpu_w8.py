@@ -279,3 +279,20 @@ def test_linear_of_each_kernel(Q, M, N, K, kernel, parts):
         Q.w8a8_linear(w, act, out=out, workspace=ws)
         assert same(out, want), dt
         assert torch.all(room[:pad] == 7) and torch.all(room[pad + M * N:] == 7)
+
+
+def test_one_workspace_for_a_servers_steps(Q):
+    """Steps of any size one after the other in the workspace of all sizes, dirty from the step before."""
+    rng = np.random.default_rng(23)
+    N, K, most = 1027, 8256, 400
+    L, q, s_w, s_x = operands(rng, N, K, most)
+    w = Q.W8(dev(L), dev(s_w))
+    ws = Q.w8a8_workspace(w, range(1, most + 1))
+    acc = (q.astype(np.float64) @ L.astype(np.float64).T).astype(np.int64)
+    cut = 0
+    for M in (1, 400, 33, 130, 17, 333, 64, 399, 250):
+        cut += Q.w8a8_workspace_bytes(w, M) > 0
+        assert Q.w8a8_workspace_bytes(w, M) <= ws.numel()
+        act = Q.QAct(dev(q[:M]), dev(s_x[:M]))
+        assert same(Q.w8a8_linear(w, act, workspace=ws), expect(acc[:M], s_x[:M], s_w, torch.float16)), M
+    assert cut > 4

@@ -251,3 +251,13 @@ def test_each_kernel_has_its_sizes(tmp_path):
         assert whole and cut, tile
         assert any(c[1] % bn and c[0] % bm for c in whole) and any(c[1] % bn and c[0] % bm for c in cut), tile
         assert any(c[2] % 128 == 64 for c in whole), tile
+
+
+def test_workspace_of_several_numbers_of_tokens(L):
+    """The largest step's need is not enough for every smaller one; that of all of them is."""
+    w = object.__new__(qift.W8)
+    w.c = qift.W8C(4096, 11008, A, A)
+    w._ref = ctypes.byref(w.c)
+    each = [qift.w8a8_workspace_bytes(w, M) for M in range(1, 513)]
+    assert each[511] < max(each) and qift.w8a8_workspace_bytes(w, range(1, 513)) == max(each)
+    assert qift.w8a8_workspace_bytes(w, [333]) == each[332] and qift.w8a8_workspace_bytes(w, ()) == 0
