@@ -1,6 +1,7 @@
 /*
- * qift_w8.h - C ABI of the 8-bit linear (W8A8): the sibling of the 2- and 4-bit linears for the layers that a
- * mixed schedule (Sec. 4.4) keeps at more bits, such as the projections around the attention or the output head.
+ * qift_w8.h - C ABI of the 8-bit linear (W8A8): the sibling of the 2- and 4-bit linears for the products that a model
+ * keeps at more bits, such as the projections around the attention or the output head.  (The paper's schedules, Sec. 4.4, mix
+ * 2 and 4 bits by layer; this linear is not among them.)
  *
  *   y[m, n] = s_w[n] * s_x[m] * sum_k level[n, k] * q[m, k]
  *

@@ -50,7 +50,7 @@ __device__ __forceinline__ uint2 pack4(const float (&v)[4]) {   // to nearest, t
 // A wave takes up to 4 NG heads of one row, 16 lanes to a head; a lane has eight values as two fours, so that both values of
 // its four pairs are its own: values 4 l and rot / 2 + 4 l on (PAIRS: 8 l and 8 l + 4 on), and past the rotated ones the rest.
 // The four angles of a lane are the same for every head: lane (g, l) works out the g-th and the others read it from there.
-// Bound by the bytes, each read and written once (16384 rows of 40 heads, 671 MB, 66.4 us, 5.05 TB/s).
+// Bound by the bytes, each read and written once (16384 rows of 40 heads, 336 MB, 66.4 us, 5.05 TB/s).
 template <bool BF16, bool PAIRS, int NG>
 __global__ __launch_bounds__(256) void k_rope(RopeCall c, pages::Div per_row, uint32_t waves) {
   const int lane = threadIdx.x & 63, l = lane & 15, g = lane >> 4;
@@ -147,7 +147,7 @@ hipError_t launch_n(const RopeCall& a, hipStream_t s) {
   return hipGetLastError();
 }
 // Four heads to a wave until there are about 16 waves to each CU's SIMD; then as many as share the angles and keep loads
-// in flight, without a rest where that goes (16384 rows of 40 heads, 671 MB: 4 heads to a wave 82.7 us, 8 70.6, 16 68.4, 20 66.4,
+// in flight, without a rest where that goes (16384 rows of 40 heads, 336 MB: 4 heads to a wave 82.7 us, 8 70.6, 16 68.4, 20 66.4,
 // 32 69.2; 5.05 TB/s, a large copy's rate being 5.10.  2999 rows of 64 heads, 98 MB: 4 23.0, 16 22.5).
 template <bool BF16, bool PAIRS>
 hipError_t launch_ng(const RopeCall& a, hipStream_t s) {

@@ -2,11 +2,11 @@
 //
 // What the kernels' times follow is the bytes that a CU takes in: about 27 a ns to registers (qift_w8_rows.hip) and up to
 // 54 a ns to LDS (qift_w8_gemm.hip), whatever the matrix cores do meanwhile, and for few tokens the weights' bytes from
-// memory.  So a plan is the least of the times below (ns), which were fitted to measured ones (us, rows x K at tokens, weights
-// streamed from HBM; estimates in brackets):
-//   rows of 4: 1024 x 14336 at 1 token 7.4 (4.9; rows of 16 10.2); of 8: 2048 x 4096 4.5 (3.1; of 16 4.9); of 16: 4096 x 4096
-//     6.0 (4.7), at 32 8.6 (8.8), 28672 x 4096 at 1 24.5 (24.4), 4096 x 14336 12.9 (12.6); of 20: 10240 x 4096 11.2 (9.7; of 16
-//     12.2); of 24: 6144 x 4096 6.7 (6.2; of 16 8.9, of 32 8.1); of 40: 10000 x 2048 at 24 8.2 (7.5; of 64 9.0)
+// memory.  So a plan is the least of the times below (ns), which were fitted to measured ones (us, rows x K at tokens, 1.2 GB of
+// weights in turn, so that they come from HBM; estimates in brackets):
+//   rows of 4: 1024 x 14336 at 1 token 8.9 (4.9; rows of 16 10.5); of 8: 2048 x 4096 5.0 (3.1; of 16 5.3); of 16: 4096 x 4096
+//     5.9 (4.7), at 32 8.8 (8.8), 28672 x 4096 at 1 23.9 (24.4), 4096 x 14336 12.5 (12.6); of 20: 10240 x 4096 11.1 (9.7; of 16
+//     12.1); of 24: 6144 x 4096 7.4 (6.2; of 16 8.6, of 32 8.0); of 40: 10000 x 2048 at 24 8.2 (7.5; of 64 9.3)
 //   128 x 32 tiles: 28672 x 4096 at 16 27 to 29 (28; rows of 28 33); 128 x 64: 2500 x 4096 at 600 15 (17), 32003 x 4096 at 61 31 (32),
 //     4096 x 14336 at 64 in 8 parts 19 (23)
 //   256 x 128: 4096 x 4096 at 2048 36 (38), 4096 x 11008 at 333 in 5 parts 32 (39)
@@ -76,8 +76,8 @@ inline W8Plan w8_plan(int64_t N, int64_t M, int64_t K, bool split) {
   return best;
 }
 // Whether the rows kernel takes eight waves with units of 128 k rather than four with units of 256, for up to 16 tokens and 16
-// rows: four (4096 x 14336 at one token 12.9 us; eight 13.7; of 128 k 15.6) except where many workgroups queue for a CU
-// (28672 x 4096 24.5 with eight against 26.0).
+// rows: four (4096 x 14336 at one token 12.5 us; eight, with units of 256 too, 13.3) except where many workgroups queue for a CU
+// (28672 x 4096 23.9 with eight against 25.5).
 inline bool w8_eight_waves(const W8Plan& p, int64_t N, int64_t K) {
   return w8_ceil(N, p.rows) > 2 * kCus && K > 1024 && K <= 8192;
 }

@@ -7,14 +7,14 @@ namespace {
 using namespace w8;
 
 // A workgroup owns `own` weight rows, a multiple of 4 and at most 16 RT, and all the tokens (TT tiles of 16); `own` is chosen
-// so that the CUs have equal parts (6144 x 4096 at one token: 24 rows to each of 256 workgroups 7.2 us, 32 to 192 8.1).  Its
+// so that the CUs have equal parts (6144 x 4096 at one token: 24 rows to each of 256 workgroups 7.4 us, 32 to 192 8.0).  Its
 // waves take units of 64 U values of k in turn (unit u is wave u mod NWV's), so that together they read whole pieces of each
 // row; weights and codes go straight to the operands of the 16 x 16 x 64 product (lane (r, g): row or token r, values 16 g ..
 // 16 g + 15 of each 64), the next unit's loads sent before the present one is used.  The waves' sums meet in LDS, each wave
 // adding up and storing some of the tiles.
-// Bound by the weights' bytes with few tokens (28672 x 4096 at one 24.5 us, 4.8 TB/s; 4096 x 14336 12.9, 4.5; 4096 x 4096 6.0,
+// Bound by the weights' bytes with few tokens (28672 x 4096 at one 23.9 us, 4.9 TB/s; 4096 x 14336 12.5, 4.7; 4096 x 4096 5.9,
 // of which 2.5 are the launch and the first loads), with more by what a CU takes into registers, about 27 bytes a ns
-// (4096 x 4096 at 32 tokens 8.6 us): tiled products (qift_w8_gemm.hip) take over there.
+// (4096 x 4096 at 32 tokens 8.8 us): tiled products (qift_w8_gemm.hip) take over there.
 template <int RT, int TT, int U, int NWV, int OT>
 __global__ __launch_bounds__(64 * NWV) void k_w8_rows(const int8_t* __restrict__ W, const uint16_t* __restrict__ sw, int64_t N,
                                                       int K, int own, const int8_t* __restrict__ act, const float* __restrict__ sx,
