@@ -101,8 +101,8 @@ typedef struct {
  *   dtype       QIFT_F16 or QIFT_BF16.
  *   positions   int32 [rows].  A negative position: the row is padding, its outputs are zeros.
  *   q_out, k_out   out: as q and k, with strides of their own; the input itself with the input's stride is taken (each
- *               value is read before it is written), any other overlap is not: the same pointer with another stride, q_out
- *               at k, k_out at q or both outputs at one place are QIFT_ERR_SHAPE.
+ *               value is read before it is written), any other overlap of an output with an array of the call is
+ *               QIFT_ERR_SHAPE (rows of stacked views that lie between each other's are no overlap).
  * 16-byte aligned, positions 4.  rows = 0 does nothing.  Limits: rows * ceil((Hq + Hkv) / 4) <= 2^26 - 4.  One launch.
  */
 int qift_head_norm_rope(const qift_head_rope *rope, const void *q, int64_t q_stride, const void *k, int64_t k_stride,

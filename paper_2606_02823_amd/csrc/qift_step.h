@@ -70,6 +70,27 @@ QIFT_HD Head head_of(int32_t h, int32_t Hq, int32_t Hkv) {
   return {key ? in - Hq : in, h < all, key};
 }
 
+// Rows of `bytes` each at a stride in memory (a view of stacked rows, or one row: an array).
+struct View {
+  uint64_t at;
+  int64_t stride, bytes, rows;
+};
+// Whether two views share a byte.  Rows of one view do not overlap each other (the stride is at least a row).
+inline bool overlap(const View& a, const View& b) {
+  if (a.rows < 1 || b.rows < 1 || a.bytes < 1 || b.bytes < 1) return false;
+  const int64_t d = (int64_t)(b.at - a.at);   // of b's first row from a's
+  if (d >= (a.rows - 1) * a.stride + a.bytes || -d >= (b.rows - 1) * b.stride + b.bytes) return false;
+  // a's row i begins at x = i a.stride - d from b's first: it meets the last of b's rows that begins before it ends, or none.
+  // With one stride rows i and i + 1 lie alike, so that the first two tell.
+  for (int64_t i = d < a.bytes ? 0 : (d - a.bytes) / a.stride + 1, n = 0; i < a.rows; ++i, ++n) {
+    const int64_t x = i * a.stride - d;
+    if (x >= (b.rows - 1) * b.stride + b.bytes || (n == 2 && a.stride == b.stride)) break;
+    const int64_t below = (x + a.bytes - 1) / b.stride, j = below < b.rows ? below : b.rows - 1;
+    if (x < j * b.stride + b.bytes) return true;
+  }
+  return false;
+}
+
 // Sine and cosine of position * freq, within 2^-22 for angles below kMaxAngle; NaN from there on and for a frequency that is no
 // number.  The product is x + low exactly (55 bits at most), the remainder of x's division by pi / 2 is taken with pi / 2 in
 // two parts (off by less than 2^-51), and the Taylor sums of the remainder, |r| <= pi / 4 + 2^-12, are cut where the next term is

@@ -4,6 +4,7 @@
 
 #include "../../include/qift_step.h"
 #include "qift_internal.h"
+#include "qift_step.h"
 
 namespace {
 
@@ -94,14 +95,25 @@ int qift_head_norm_rope(const qift_head_rope* rope, const void* q, int64_t q_str
   if (!positions || (rope->rot > 0 && !rope->freq)) return QIFT_ERR_NULL;
   for (int i = 0; i < 4; ++i)
     if ((i < 2 ? Hq : Hkv) > 0 && !rowsp[i]) return QIFT_ERR_NULL;
-  // each value is read before it is written where an output is its input; other overlaps race
-  if (rows > 1 && ((Hq > 0 && q == q_out && q_stride != q_out_stride) || (Hkv > 0 && k == k_out && k_stride != k_out_stride)))
-    return QIFT_ERR_SHAPE;
-  if (Hq > 0 && Hkv > 0 && (q_out == k || k_out == q || q_out == k_out)) return QIFT_ERR_SHAPE;
   for (int i = 0; i < 4; ++i)
     if ((i < 2 ? Hq : Hkv) > 0 && (!aligned(rowsp[i], 16) || strides[i] % 8)) return QIFT_ERR_ALIGN;
   if (!aligned(positions, 4) || !aligned(rope->freq, 16) || !aligned(rope->q_weight, 16) || !aligned(rope->k_weight, 16))
     return QIFT_ERR_ALIGN;
+  // each value is read before it is written where an output is its input; any other overlap of what is written races
+  auto view = [](const void* p, int64_t stride, int64_t bytes, int64_t n) {
+    return qift::step::View{reinterpret_cast<uintptr_t>(p), stride, bytes, n};
+  };
+  qift::step::View v[8];
+  for (int i = 0; i < 4; ++i) v[i] = view(rowsp[i], 2 * strides[i], (i < 2 ? Hq : Hkv) * 256, rows);
+  v[4] = view(positions, 4 * rows, 4 * rows, 1);
+  v[5] = view(rope->freq, 256, rope->rot * 2, 1);
+  v[6] = view(rope->q_weight, 256, rope->q_weight ? 256 : 0, 1);
+  v[7] = view(rope->k_weight, 256, rope->k_weight ? 256 : 0, 1);
+  for (int out = 1; out < 4; out += 2)
+    for (int i = 0; i < 8; ++i) {
+      const bool in_place = i == out - 1 && v[i].at == v[out].at && (rows == 1 || v[i].stride == v[out].stride);
+      if (i != out && !in_place && qift::step::overlap(v[out], v[i])) return QIFT_ERR_SHAPE;
+    }
   qift::RopeCall c;
   c.x[0] = static_cast<const uint16_t*>(q);
   c.x[1] = static_cast<const uint16_t*>(k);

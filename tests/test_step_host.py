@@ -354,3 +354,61 @@ def test_rope_launches_have_fewer_than_2_32_threads(L):
     for rows in (2 ** 26 - 3, 2 ** 26 - 1):
         for Hq in (1, 4):
             assert L.qift_head_norm_rope(ctypes.byref(r), A, 512, None, 0, 0, A, rows, Hq, 0, A, 512, None, 0, None) == E_SHAPE
+
+
+VIEWS = r"""
+#include <cstdio>
+#include "qift_step.h"
+int main() {
+  long v[8];
+  for (;;) {
+    for (long& x : v)
+      if (std::scanf("%ld", &x) != 1) return 0;
+    using qift::step::View;
+    std::printf("%d\n", (int)qift::step::overlap(View{(unsigned long)v[0], v[1], v[2], v[3]}, View{(unsigned long)v[4], v[5], v[6], v[7]}));
+  }
+}
+"""
+
+
+def test_views_that_share_memory(tmp_path):
+    """Against the bytes one by one: any strides, interleaved rows of one stride, ends that touch, single rows, none."""
+    cxx = shutil.which("g++") or shutil.which("clang++") or "/opt/rocm/llvm/bin/clang++"
+    (tmp_path / "probe.cpp").write_text(VIEWS)
+    subprocess.run([cxx, "-std=c++17", "-I", CSRC, str(tmp_path / "probe.cpp"), "-o", str(tmp_path / "probe")], check=True)
+    rng = np.random.default_rng(11)
+    cases = []
+    for i in range(20000):
+        view = []
+        for _ in range(2):
+            size = int(rng.integers(0, 6))
+            view.append([int(rng.integers(1000, 1060)), size + int(rng.integers(0, 9)) + (size == 0), size, int(rng.integers(0, 7))])
+        if i % 2:
+            view[1][1] = view[0][1] = max(view[0][1], view[1][1])     # one stride
+        cases.append(view)
+    out = subprocess.run([str(tmp_path / "probe")], input="\n".join(" ".join(map(str, a + b)) for a, b in cases), text=True,
+                         capture_output=True, check=True).stdout.split()
+    assert len(out) == len(cases)
+    seen = [0, 0]
+    for (a, b), got in zip(cases, out):
+        sets = [{at + r * stride + i for r in range(rows) for i in range(size)} for at, stride, size, rows in (a, b)]
+        assert int(got) == bool(sets[0] & sets[1]), (a, b)
+        seen[int(got)] += 1
+    assert min(seen) > 3000
+
+
+def test_rope_outputs_lie_apart(L):
+    """Waves take their heads in any order: an output is its own input with its stride, or shares nothing with any array."""
+    r = qift.HeadRopeC(128, 128, 0, 1e-5, 0x1000, 0x1400, 0x1800)
+    rows, s = 40, 48 * 128      # q, k and v of 32 + 8 + 8 heads stacked
+    big = 0x1000000
+
+    def f(q=big, qs=s, k=big + 2 * 32 * 128, ks=s, pos=0x2000, qo=2 * big, qos=32 * 128, ko=3 * big, kos=8 * 128):
+        return L.qift_head_norm_rope(ctypes.byref(r), q, qs, k, ks, 0, pos, rows, 32, 8, qo, qos, ko, kos, None)
+
+    row, head = 2 * s, 256
+    for kw in ({"qo": big + head, "qos": s}, {"qo": big - head, "qos": s}, {"qo": big + row, "qos": s}, {"qo": big + row, "qos": 2 * s},
+               {"qo": big + 39 * row}, {"ko": big + 31 * head, "kos": s}, {"ko": big + 33 * head, "kos": s}, {"ko": big + 5 * row + 39 * head},
+               {"ko": big, "kos": s}, {"qo": 2 * big, "ko": 2 * big + 31 * head, "qos": s, "kos": s}, {"ko": 2 * big + 39 * 32 * head},
+               {"qo": 0x2000}, {"qo": 0x2000 + 144}, {"ko": 0x1000}, {"ko": 0x1400 + 240}, {"ko": 0x1800}):
+        assert f(**kw) == E_SHAPE, kw
